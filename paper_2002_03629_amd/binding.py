@@ -22,6 +22,7 @@ EXPORTS = ["made_init", "made_conv_init", "made_free", "made_forward_logits", "m
            "jacobi_sample_real", "gs_jacobi_sample_real", "made_last_stats", "made_set_profiling", "made_last_profile", "made_set_option",
            "made_layer_nnz",
            "rnn_forward", "rnn_backward_sequential", "rnn_backward_jacobi", "rnn_jacobi_max_steps", "rnn_param_grads",
+           "linattn_workspace_bytes", "linattn_forward", "linattn_backward", "linattn_step",
            "made_last_error"]
 
 
@@ -39,6 +40,12 @@ class made_config(C.Structure):
 class made_conv_config(C.Structure):
     _fields_ = [("H", C.c_int32), ("W", C.c_int32), ("C", C.c_int32), ("F", C.c_int32), ("k", C.c_int32),
                 ("n_conv", C.c_int32), ("dtype", C.c_int32)]
+
+
+class linattn_config(C.Structure):
+    _fields_ = [("B", C.c_int32), ("T", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("Dk", C.c_int32),
+                ("Dv", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("ld_q", C.c_int64), ("ld_k", C.c_int64),
+                ("ld_v", C.c_int64), ("ld_o", C.c_int64), ("offsets", C.c_void_p)]
 
 
 _lib = None
@@ -82,6 +89,11 @@ def lib() -> C.CDLL:
         L.rnn_backward_jacobi.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, C.c_float, vp, vp, vp, vp]
         L.rnn_jacobi_max_steps.argtypes = [i32]
         L.rnn_param_grads.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]
+        cfg = C.POINTER(linattn_config)
+        L.linattn_workspace_bytes.argtypes = [cfg, i32, i64p]
+        L.linattn_forward.argtypes = [cfg] + [vp] * 8 + [C.c_int64, vp]
+        L.linattn_backward.argtypes = [cfg] + [vp] * 12 + [C.c_int64, vp]
+        L.linattn_step.argtypes = [cfg] + [vp] * 5 + [i32, vp, vp, vp]
         L.made_last_error.argtypes = []
         L.made_last_error.restype = C.c_char_p
         for name in EXPORTS[:-1]:
@@ -367,3 +379,168 @@ def rnn_param_grads(z, h, x, d, h0, B: int, T: int, H: int, I: int, dW, dU, db, 
     f = torch.float32
     _check(lib().rnn_param_grads(_ptr(z, f), _ptr(h, f), _ptr(x, f), _ptr(d, f), _ptr(h0, f), B, T, H, I, _ptr(dW, f),
                                  _ptr(dU, f), _ptr(db, f), _stream(stream)))
+
+
+# ------------------------------------------------------------------------------------------------
+# linear attention with a decay for each head (include/jacobi_linattn.h).  q, k, v, o and their gradients are float32 or
+# bfloat16 (all the same), [B, T, heads, D] or, packed (offsets given), [T, heads, D]; the heads of a step are contiguous,
+# the steps may lie further apart (parts of a wider tensor).  States and log_decay are float32.
+# ------------------------------------------------------------------------------------------------
+def _on_device(t, what: str, stream=None):
+    """A tensor that a kernel on the current device (of `stream`, if one is given) may be handed."""
+    import torch
+    if not t.is_cuda:
+        raise ValueError(f"{what} is not on the GPU")
+    device = torch.cuda.current_device() if stream is None else stream.device.index
+    if t.device.index != device:
+        raise ValueError(f"{what} is on cuda:{t.device.index}, the call is for cuda:{device}")
+    return t
+
+
+def _dense(t, what: str, shape, dtype, stream=None) -> Optional[int]:
+    """Device pointer of a contiguous tensor of that shape and type (or None)."""
+    if t is None:
+        return None
+    _on_device(t, what, stream)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return _ptr(t, dtype)
+
+
+def _rows(t, what: str, lead, heads: int, D: int, dtype, stream=None):
+    """(device pointer, elements from row to row) of [*lead, heads, D] whose rows are contiguous and equally far apart."""
+    _on_device(t, what, stream)
+    if tuple(t.shape) != tuple(lead) + (heads, D):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(lead) + (heads, D)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    if t.numel() == 0:
+        return None, 0
+    st = t.stride()
+    if (D > 1 and st[-1] != 1) or (heads > 1 and st[-2] != D):
+        raise ValueError(f"{what}: the heads of a row must be contiguous")
+    wide = heads * D
+    if len(lead) == 1:
+        ld = st[0] if lead[0] > 1 else wide
+    elif lead[1] > 1:
+        ld = st[1]
+        if lead[0] > 1 and st[0] != ld * lead[1]:
+            raise ValueError(f"{what}: the rows must be equally far apart")
+    else:
+        ld = st[0] if lead[0] > 1 else wide
+    if ld < wide:
+        raise ValueError(f"{what}: rows overlap")
+    return t.data_ptr(), ld
+
+
+def _linattn_dtype(q) -> int:
+    import torch
+    if q.dtype == torch.float32:
+        return MADE_F32
+    if q.dtype == torch.bfloat16:
+        return MADE_BF16
+    raise ValueError(f"expected torch.float32 or torch.bfloat16, got {q.dtype}")
+
+
+def linattn_workspace_bytes(B: int, T: int, heads: int, kv_heads: int, Dk: int, Dv: int, dtype, packed: bool = False,
+                            backward: bool = False) -> int:
+    """dtype: torch.float32 or torch.bfloat16."""
+    import torch
+    cfg = linattn_config(int(B), int(T), int(heads), int(kv_heads), int(Dk), int(Dv),
+                         MADE_BF16 if dtype == torch.bfloat16 else MADE_F32, 1.0, 0, 0, 0, 0, 1 if packed else None)
+    out = C.c_int64()
+    _check(lib().linattn_workspace_bytes(C.byref(cfg), 1 if backward else 0, C.byref(out)))
+    return out.value
+
+
+def _linattn_args(q, k, v, log_decay, offsets, B, T, heads, kv_heads, Dk, Dv, scale, o, stream):
+    import torch
+    lead = (B, T) if offsets is None else (T,)
+    dt = q.dtype
+    code = _linattn_dtype(q)
+    pq, lq = _rows(q, "q", lead, heads, Dk, dt, stream)
+    pk, lk = _rows(k, "k", lead, kv_heads, Dk, dt, stream)
+    pv, lv = _rows(v, "v", lead, kv_heads, Dv, dt, stream)
+    po, lo = _rows(o, "o", lead, heads, Dv, dt, stream)
+    cfg = linattn_config(int(B), int(T), int(heads), int(kv_heads), int(Dk), int(Dv), code, float(scale), lq, lk, lv, lo,
+                         _dense(offsets, "offsets", (B + 1,), torch.int32, stream))
+    return cfg, pq, pk, pv, po, _dense(log_decay, "log_decay", (kv_heads,), torch.float32, stream)
+
+
+def _linattn_workspace(cfg, backward: bool, workspace, stream):
+    """The workspace given, or one of torch's allocator's on the stream of the call."""
+    import torch
+    if workspace is None:
+        need = C.c_int64()
+        _check(lib().linattn_workspace_bytes(C.byref(cfg), 1 if backward else 0, C.byref(need)))
+        if need.value == 0:
+            return None, 0, None
+        with torch.cuda.stream(stream):          # (None: the current one)
+            workspace = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+    else:
+        _on_device(workspace, "workspace", stream)
+    return _ptr(workspace, torch.uint8), workspace.numel(), workspace
+
+
+def linattn_forward(q, k, v, log_decay, state_in, offsets, B: int, T: int, heads: int, kv_heads: int, Dk: int, Dv: int,
+                    scale: float, o, state_out=None, workspace=None, stream=None) -> None:
+    """workspace: uint8, of linattn_workspace_bytes(...) bytes, used by one call at a time; None: taken for the call."""
+    import torch
+    f = torch.float32
+    cfg, pq, pk, pv, po, pd = _linattn_args(q, k, v, log_decay, offsets, B, T, heads, kv_heads, Dk, Dv, scale, o, stream)
+    shape = (B, kv_heads, Dk, Dv)
+    ws, ws_bytes, keep = _linattn_workspace(cfg, False, workspace, stream)
+    _check(lib().linattn_forward(C.byref(cfg), pq, pk, pv, pd, _dense(state_in, "state_in", shape, f, stream), po,
+                                 _dense(state_out, "state_out", shape, f, stream), ws, ws_bytes, _stream(stream)))
+
+
+def linattn_backward(q, k, v, log_decay, state_in, offsets, d_o, d_state_out, B: int, T: int, heads: int, kv_heads: int,
+                     Dk: int, Dv: int, scale: float, dq, dk, dv, d_state_in=None, workspace=None, stream=None) -> None:
+    import torch
+    f = torch.float32
+    cfg, pq, pk, pv, pdo, pd = _linattn_args(q, k, v, log_decay, offsets, B, T, heads, kv_heads, Dk, Dv, scale, d_o, stream)
+    lead = (B, T) if offsets is None else (T,)
+    grads = []
+    for t, what, n, D, ld in ((dq, "dq", heads, Dk, cfg.ld_q), (dk, "dk", kv_heads, Dk, cfg.ld_k), (dv, "dv", kv_heads, Dv, cfg.ld_v)):
+        p, own = _rows(t, what, lead, n, D, q.dtype, stream)
+        if own != ld:
+            raise ValueError(f"{what} must have the row stride of {what[1:]} ({ld}), has {own}")
+        grads.append(p)
+    shape = (B, kv_heads, Dk, Dv)
+    ws, ws_bytes, keep = _linattn_workspace(cfg, True, workspace, stream)
+    _check(lib().linattn_backward(C.byref(cfg), pq, pk, pv, pd, _dense(state_in, "state_in", shape, f, stream), pdo,
+                                  _dense(d_state_out, "d_state_out", shape, f, stream), *grads,
+                                  _dense(d_state_in, "d_state_in", shape, f, stream), ws, ws_bytes, _stream(stream)))
+
+
+class PreparedLinattnStep:
+    """linattn_step with its arguments marshalled once, for loops that generate step after step on the same buffers: calling
+    the object runs the step.  The tensors are kept alive; their contents may change between calls."""
+
+    def __init__(self, q, k, v, log_decay, state, slots, B: int, heads: int, kv_heads: int, Dk: int, Dv: int, scale: float, o,
+                 stream=None):
+        import torch
+        code = _linattn_dtype(q)
+        pq, lq = _rows(q, "q", (B,), heads, Dk, q.dtype, stream)
+        pk, lk = _rows(k, "k", (B,), kv_heads, Dk, q.dtype, stream)
+        pv, lv = _rows(v, "v", (B,), kv_heads, Dv, q.dtype, stream)
+        po, lo = _rows(o, "o", (B,), heads, Dv, q.dtype, stream)
+        n_slots = state.shape[0]
+        self._keep = (q, k, v, log_decay, state, slots, o, stream)
+        self._cfg = linattn_config(int(B), 1, int(heads), int(kv_heads), int(Dk), int(Dv), code, float(scale), lq, lk, lv, lo, None)
+        self._fn = lib().linattn_step
+        vp = C.c_void_p
+        self._args = (C.byref(self._cfg), vp(pq), vp(pk), vp(pv), vp(_dense(log_decay, "log_decay", (kv_heads,), torch.float32, stream)),
+                      vp(_dense(state, "state", (n_slots, kv_heads, Dk, Dv), torch.float32, stream)), C.c_int32(n_slots),
+                      vp(_dense(slots, "slots", (B,), torch.int32, stream)), vp(po), vp(_stream(stream)))
+
+    def __call__(self) -> None:
+        code = self._fn(*self._args)
+        if code != MADE_OK:
+            raise MadeError(code, made_last_error())
+
+
+def linattn_step(q, k, v, log_decay, state, slots, B: int, heads: int, kv_heads: int, Dk: int, Dv: int, scale: float, o,
+                 stream=None) -> None:
+    """state [n_slots, kv_heads, Dk, Dv] is updated in place; slots: int32 [B] or None (row b has place b)."""
+    PreparedLinattnStep(q, k, v, log_decay, state, slots, B, heads, kv_heads, Dk, Dv, scale, o, stream)()

@@ -7,11 +7,12 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libjacobi_made.so")
-SOURCES = ["jacobi_made.hip"]
+SOURCES = ["jacobi_made.hip", "linattn.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-pthread", "-Wall", "-Wno-unused-function",
     # keep the compiler from forming packed-fp32 instructions
@@ -19,18 +20,31 @@ FLAGS = [
 ]
 
 
+def _run_all(cmds, verbose: bool) -> None:
+    """Runs the commands at once, waits for all of them and prints or raises what they said."""
+    procs = []
+    for cmd in cmds:
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        procs.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+    outs = [p.communicate()[0] for p in procs]
+    for p, text in zip(procs, outs):
+        text = "\n".join(l for l in text.splitlines() if "packed-fp32-ops" not in l)
+        if p.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + text)
+        if verbose and text.strip():
+            print(text)
+
+
 def build_library(verbose: bool = True, out_path: str = LIB_PATH, defines=(), extra_flags=()) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = ([hipcc] + FLAGS + list(extra_flags) + ["-D" + d for d in defines] + [os.path.join(CSRC, s) for s in SOURCES] +
-           ["-o", out_path])
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(l for l in proc.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if proc.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
-    if verbose and out.strip():
-        print(out)
+    flags = [hipcc] + FLAGS + list(extra_flags)
+    with tempfile.TemporaryDirectory() as tmp:
+        # every source for itself, all at once; then the link
+        objects = [os.path.join(tmp, s.replace(".hip", ".o")) for s in SOURCES]
+        steps = [flags + ["-D" + d for d in defines] + ["-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objects)]
+        _run_all([[a for a in cmd if a != "-shared"] for cmd in steps], verbose)
+        _run_all([flags + objects + ["-o", out_path]], verbose)
     return out_path
 
 

@@ -23,6 +23,7 @@
 #include <thread>
 #include <vector>
 
+#include "entry.hpp"
 #include "kernels.hpp"
 #include "resident.hpp"
 #include "onehot.hpp"
@@ -62,31 +63,15 @@ static hipError_t scratch_address(int device, void** out) {
 // ------------------------------------------------------------------------------------------------
 // errors
 // ------------------------------------------------------------------------------------------------
-static thread_local std::string g_last_error;
+static thread_local char g_last_error[512] = "";
 
-static int fail(int code, const char* fmt, ...) {
-  char buf[512];
+int jm::fail(int code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
+  vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
   va_end(ap);
-  g_last_error = buf;
   return code;
 }
-
-#define HIP_TRY(expr)                                                                               \
-  do {                                                                                              \
-    hipError_t e_ = (expr);                                                                         \
-    if (e_ != hipSuccess)                                                                           \
-      return fail(e_ == hipErrorOutOfMemory ? MADE_ERR_NOMEM : MADE_ERR_HIP, "%s failed: %s (%s:%d)", #expr, \
-                  hipGetErrorString(e_), __FILE__, __LINE__);                                       \
-  } while (0)
-
-#define TRY(expr)            \
-  do {                       \
-    int rc_ = (expr);        \
-    if (rc_ != MADE_OK) return rc_; \
-  } while (0)
 
 static inline int round_up(int v, int m) { return (v + m - 1) / m * m; }
 
@@ -532,7 +517,7 @@ extern "C" int made_free(made_model* m) {
   return MADE_OK;
 }
 
-extern "C" const char* made_last_error(void) { return g_last_error.c_str(); }
+extern "C" const char* made_last_error(void) { return g_last_error; }
 
 extern "C" int made_last_stats(const made_model* m, int64_t* out, int32_t n) {
   if (!m || !out || n < 0) return fail(MADE_ERR_ARG, "made_last_stats: NULL argument");

@@ -1,0 +1,330 @@
+// Host side of the linear-attention entry points (include/jacobi_linattn.h).
+#include "../../include/jacobi_linattn.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "entry.hpp"
+#include "linattn.hpp"
+
+using namespace jm;
+
+namespace {
+
+constexpr int SPLIT_TARGET = 512;      // workgroups that fill the device: two to a compute unit
+
+int block_rows(const linattn_config& c) { return c.dtype == MADE_BF16 ? LaShape<la_bf16>::C : LaShape<float>::C; }
+
+int check(const char* who, const linattn_config* c, bool step) {
+  if (!c) return fail(MADE_ERR_ARG, "%s: NULL config", who);
+  if (c->B < 0 || (!step && c->T < 0)) return fail(MADE_ERR_ARG, "%s: B=%d, T=%d out of range", who, c->B, c->T);
+  if (c->Dk < 1 || c->Dv < 1 || c->Dk > LA_MAX_D || c->Dv > LA_MAX_D)
+    return fail(MADE_ERR_ARG, "%s: Dk=%d, Dv=%d, widths of 1 to %d are supported", who, c->Dk, c->Dv, LA_MAX_D);
+  if (c->kv_heads < 1 || c->heads < 1 || c->heads % c->kv_heads != 0)
+    return fail(MADE_ERR_ARG, "%s: heads=%d must be a positive multiple of kv_heads=%d", who, c->heads, c->kv_heads);
+  if (c->dtype != MADE_F32 && c->dtype != MADE_BF16) return fail(MADE_ERR_ARG, "%s: dtype=%d is neither MADE_F32 nor MADE_BF16", who, c->dtype);
+  const int64_t need[4] = {(int64_t)c->heads * c->Dk, (int64_t)c->kv_heads * c->Dk, (int64_t)c->kv_heads * c->Dv, (int64_t)c->heads * c->Dv};
+  const int64_t ld[4] = {c->ld_q, c->ld_k, c->ld_v, c->ld_o};
+  for (int i = 0; i < 4; ++i) {
+    if (std::max(ld[i], need[i]) > LA_MAX_LD)
+      return fail(MADE_ERR_ARG, "%s: rows of %c are %lld elements apart, at most %d are supported", who, "qkvo"[i],
+                  (long long)std::max(ld[i], need[i]), LA_MAX_LD);
+    if (ld[i] != 0 && ld[i] < need[i])
+      return fail(MADE_ERR_ARG, "%s: row stride %lld of %c is shorter than a row (%lld)", who, (long long)ld[i], "qkvo"[i], (long long)need[i]);
+  }
+  if (!std::isfinite(c->scale)) return fail(MADE_ERR_ARG, "%s: scale is not finite", who);
+  return MADE_OK;
+}
+
+// How a call's sequences are cut.  rows: of a segment; slots: segments in all.
+struct Split {
+  int rows, slots;
+  bool on;
+};
+
+// One workgroup for each head of a sequence, unless those fill less than the device: then the sequences are cut into
+// segments, whose sums and entering states take another pass over keys and values and two more launches.
+Split choose(const linattn_config& c, int roles) {
+  const int C = block_rows(c);
+  const long long blocks = ((long long)c.T + C - 1) / C;     // of the longest sequence there may be
+  const long long units = (long long)c.kv_heads * roles;
+  const long long seqs = c.B;
+  const int whole_rows = (int)std::min<long long>(std::max<long long>(blocks, 1) * C, 0x7fffffff / C * C);
+  Split whole = {whole_rows, c.B, false};
+  if (blocks <= 1) return whole;
+  auto slots = [&](long long L) { return c.offsets ? blocks / L + seqs : (blocks + L - 1) / L * seqs; };
+  auto rounds = [&](long long n) { return (double)std::max<long long>(1, (n * units + SPLIT_TARGET - 1) / SPLIT_TARGET); };
+  double best = rounds(seqs) * blocks;
+  long long best_l = blocks;
+  for (long long L = 1; L < blocks; L = L < 8 ? L + 1 : L + L / 4) {
+    const double cost = rounds(slots(L)) * L * 1.5 + 8.0;
+    if (cost < best) {
+      best = cost;
+      best_l = L;
+    }
+  }
+  if (best_l >= blocks) return whole;
+  Split s = {(int)(best_l * C), (int)slots(best_l), true};
+  return s;
+}
+
+long long state_floats(const linattn_config& c, const Split& s) { return s.on ? (long long)s.slots * c.kv_heads * c.Dk * c.Dv : 0; }
+
+LinattnView view(const void* p, int64_t ld, int heads, int dim, int dtype) {
+  const int size = dtype == MADE_BF16 ? 2 : 4;
+  LinattnView v;
+  v.p = const_cast<void*>(p);
+  v.ld = ld ? ld : (int64_t)heads * dim;
+  v.dim = dim;
+  v.vec = (uintptr_t)p % 16 == 0 && v.ld * size % 16 == 0 && dim * size % 16 == 0;
+  return v;
+}
+
+int tiles(int d) { return d <= 32 ? 1 : d <= 64 ? 2 : 4; }
+
+template <typename T, int KT, int VT>
+void launch_walk(const LinattnArgs& a, bool out, hipStream_t s) {
+  const long long units = (long long)a.slots * a.kv_heads;
+  const dim3 grid((unsigned)((units + 7) / 8 * 8 * a.roles));
+  if (out) hipLaunchKernelGGL((linattn_walk_kernel<T, KT, VT, true>), grid, dim3(64 * VT), 0, s, a);
+  else hipLaunchKernelGGL((linattn_walk_kernel<T, KT, VT, false>), grid, dim3(64 * VT), 0, s, a);
+}
+
+template <typename T, int KT>
+void launch_walk(int vt, const LinattnArgs& a, bool out, hipStream_t s) {
+  switch (vt) {
+    case 1: return launch_walk<T, KT, 1>(a, out, s);
+    case 2: return launch_walk<T, KT, 2>(a, out, s);
+    default: return launch_walk<T, KT, 4>(a, out, s);
+  }
+}
+
+template <typename T>
+void launch_walk(int kt, int vt, const LinattnArgs& a, bool out, hipStream_t s) {
+  switch (kt) {
+    case 1: return launch_walk<T, 1>(vt, a, out, s);
+    case 2: return launch_walk<T, 2>(vt, a, out, s);
+    default: return launch_walk<T, 4>(vt, a, out, s);
+  }
+}
+
+void launch_walk(int dtype, const LinattnArgs& a, bool out, hipStream_t s) {
+  const int kt = tiles(a.role[0].dk), vt = tiles(a.role[0].dv);
+  if (dtype == MADE_BF16) launch_walk<la_bf16>(kt, vt, a, out, s);
+  else launch_walk<float>(kt, vt, a, out, s);
+}
+
+void launch_join(const LinattnArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(linattn_join_kernel, dim3((a.role[0].dk * a.role[0].dv + 255) / 256, a.kv_heads, a.B * a.roles), dim3(256), 0, s, a);
+}
+
+LinattnArgs common(const linattn_config& c, const float* log_decay, const Split& s) {
+  LinattnArgs a;
+  memset(&a, 0, sizeof a);
+  a.log_decay = log_decay;
+  a.offsets = c.offsets;
+  a.B = c.B;
+  a.T = c.T;
+  a.kv_heads = c.kv_heads;
+  a.seg_rows = s.rows;
+  a.slots = s.slots;
+  return a;
+}
+
+// A workspace that is too small is none; `split` becomes the uncut call then.
+int take_workspace(const char* who, const linattn_config& c, void* workspace, int64_t bytes, int sets, Split& split) {
+  if (workspace && (uintptr_t)workspace % 256 != 0) return fail(MADE_ERR_ARG, "%s: the workspace is not 256-byte aligned", who);
+  const long long need = state_floats(c, split) * 4 * sets;
+  if (split.on && (!workspace || bytes < need)) {
+    const int C = block_rows(c);
+    split.rows = (int)std::min<long long>(((long long)c.T + C - 1) / C * C, 0x7fffffff / C * C);
+    split.slots = c.B;
+    split.on = false;
+  }
+  return MADE_OK;
+}
+
+int check_grid(const char* who, const linattn_config& c, const Split& s, int roles) {
+  if (((long long)s.slots * c.kv_heads + 7) * roles > 0x7fffffffLL || (long long)c.B * roles > 65535)
+    return fail(MADE_ERR_ARG, "%s: B=%d, heads=%d are more than one launch takes", who, c.B, c.kv_heads);
+  return MADE_OK;
+}
+
+}  // namespace
+
+extern "C" int linattn_workspace_bytes(const linattn_config* cfg, int32_t backward, int64_t* bytes) {
+  if (!bytes) return fail(MADE_ERR_ARG, "linattn_workspace_bytes: NULL argument");
+  TRY(check("linattn_workspace_bytes", cfg, false));
+  *bytes = state_floats(*cfg, choose(*cfg, backward ? 3 : 1)) * 4 * (backward ? 2 : 1);
+  return MADE_OK;
+}
+
+extern "C" int linattn_forward(const linattn_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
+                               const float* state_in, void* o, float* state_out, void* workspace, int64_t workspace_bytes,
+                               void* stream) {
+  const char* who = "linattn_forward";
+  TRY(check(who, cfg, false));
+  const linattn_config& c = *cfg;
+  if (c.B == 0) return MADE_OK;
+  if (!log_decay || (c.T > 0 && (!q || !k || !v || !o))) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
+  Split split = choose(c, 1);
+  TRY(take_workspace(who, c, workspace, workspace_bytes, 1, split));
+  TRY(check_grid(who, c, split, 1));
+  hipStream_t s = (hipStream_t)stream;
+  LinattnArgs a = common(c, log_decay, split);
+  a.roles = 1;
+  LinattnRole& r = a.role[0];
+  r.q = view(q, c.ld_q, c.heads, c.Dk, c.dtype);
+  r.k = view(k, c.ld_k, c.kv_heads, c.Dk, c.dtype);
+  r.v = view(v, c.ld_v, c.kv_heads, c.Dv, c.dtype);
+  r.o = view(o, c.ld_o, c.heads, c.Dv, c.dtype);
+  r.start = state_in;
+  r.end = state_out;
+  r.seg = split.on ? (float*)workspace : nullptr;
+  r.dk = c.Dk;
+  r.dv = c.Dv;
+  r.st_r = c.Dv;
+  r.st_c = 1;
+  r.gq = c.heads / c.kv_heads;
+  r.gk = 1;
+  r.parts = state_out ? 3 : 1;
+  r.p_scale = r.i_scale = c.scale;
+  r.s_scale = 1.0f;
+  if (split.on) {
+    launch_walk(c.dtype, a, false, s);
+    launch_join(a, s);
+  }
+  launch_walk(c.dtype, a, true, s);
+  HIP_TRY(hipGetLastError());
+  return MADE_OK;
+}
+
+extern "C" int linattn_backward(const linattn_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
+                                const float* state_in, const void* d_o, const float* d_state_out, void* dq, void* dk, void* dv,
+                                float* d_state_in, void* workspace, int64_t workspace_bytes, void* stream) {
+  const char* who = "linattn_backward";
+  TRY(check(who, cfg, false));
+  const linattn_config& c = *cfg;
+  if (c.B == 0) return MADE_OK;
+  if (!log_decay || (c.T > 0 && (!q || !k || !v || !d_o || !dq || !dk || !dv))) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
+  if (d_state_in && d_state_in == d_state_out) return fail(MADE_ERR_ARG, "%s: d_state_in is d_state_out", who);
+  Split split = choose(c, 3);
+  TRY(take_workspace(who, c, workspace, workspace_bytes, 2, split));
+  TRY(check_grid(who, c, split, 3));
+  hipStream_t s = (hipStream_t)stream;
+  const int G = c.heads / c.kv_heads;
+  const LinattnView vq = view(q, c.ld_q, c.heads, c.Dk, c.dtype), vk = view(k, c.ld_k, c.kv_heads, c.Dk, c.dtype),
+                    vv = view(v, c.ld_v, c.kv_heads, c.Dv, c.dtype), vdo = view(d_o, c.ld_o, c.heads, c.Dv, c.dtype);
+  float* seg_s = split.on ? (float*)workspace : nullptr;
+  float* seg_r = split.on ? seg_s + state_floats(c, split) : nullptr;
+  LinattnRole S, R;                                   // the states forward, and their gradients back in time
+  memset(&S, 0, sizeof S);
+  S.k = vk;
+  S.v = vv;
+  S.start = state_in;
+  S.seg = seg_s;
+  S.dk = c.Dk;
+  S.dv = c.Dv;
+  S.st_r = c.Dv;
+  S.st_c = 1;
+  S.gq = S.gk = 1;
+  S.parts = 1;
+  S.p_scale = S.i_scale = c.scale;
+  S.s_scale = 1.0f;
+  R = S;
+  R.q = vk;                                           // (as the role of dv)
+  R.k = vq;
+  R.v = vdo;
+  R.o = view(dv, c.ld_v, c.kv_heads, c.Dv, c.dtype);
+  R.start = d_state_out;
+  R.end = d_state_in;
+  R.seg = seg_r;
+  R.gk = G;
+  R.back = 1;
+  R.parts = d_state_in ? 3 : 1;
+  R.i_scale = 1.0f;
+  R.s_scale = c.scale;
+  LinattnArgs a = common(c, log_decay, split);
+  if (split.on) {
+    a.roles = 2;
+    a.role[0] = S;
+    a.role[1] = R;
+    launch_walk(c.dtype, a, false, s);
+    launch_join(a, s);
+  }
+  LinattnRole Q = S, K = R;                           // dq: the states forward, transposed; dk: their gradients, transposed
+  Q.q = vdo;
+  Q.k = vv;
+  Q.v = vk;
+  Q.o = view(dq, c.ld_q, c.heads, c.Dk, c.dtype);
+  Q.gq = G;
+  K.q = vv;
+  K.k = vdo;
+  K.v = vq;
+  K.o = view(dk, c.ld_k, c.kv_heads, c.Dk, c.dtype);
+  K.end = nullptr;
+  K.parts = 1;
+  Q.dk = K.dk = c.Dv;
+  Q.dv = K.dv = c.Dk;
+  Q.st_r = K.st_r = 1;
+  Q.st_c = K.st_c = c.Dv;
+  a.role[0] = Q;
+  a.role[1] = K;
+  a.role[2] = R;
+  if (tiles(c.Dk) == tiles(c.Dv)) {
+    a.roles = 3;
+    launch_walk(c.dtype, a, true, s);
+  } else {
+    a.roles = 2;
+    launch_walk(c.dtype, a, true, s);
+    a.roles = 1;
+    a.role[0] = R;
+    launch_walk(c.dtype, a, true, s);
+  }
+  HIP_TRY(hipGetLastError());
+  return MADE_OK;
+}
+
+extern "C" int linattn_step(const linattn_config* cfg, const void* q, const void* k, const void* v, const float* log_decay,
+                            float* state, int32_t n_slots, const int32_t* slots, void* o, void* stream) {
+  const char* who = "linattn_step";
+  TRY(check(who, cfg, true));
+  const linattn_config& c = *cfg;
+  if (n_slots < 0 || (!slots && n_slots < c.B)) return fail(MADE_ERR_ARG, "%s: n_slots=%d, B=%d", who, n_slots, c.B);
+  if (c.B == 0) return MADE_OK;
+  if (!q || !k || !v || !log_decay || !state || !o) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
+  LinattnStepArgs a;
+  a.q = view(q, c.ld_q, c.heads, c.Dk, c.dtype);
+  a.k = view(k, c.ld_k, c.kv_heads, c.Dk, c.dtype);
+  a.v = view(v, c.ld_v, c.kv_heads, c.Dv, c.dtype);
+  a.o = view(o, c.ld_o, c.heads, c.Dv, c.dtype);
+  a.log_decay = log_decay;
+  a.state = state;
+  a.slots = slots;
+  a.n_slots = n_slots;
+  a.B = c.B;
+  a.kv_heads = c.kv_heads;
+  a.group = c.heads / c.kv_heads;
+  a.dk = c.Dk;
+  a.dv = c.Dv;
+  a.scale = c.scale;
+  a.vec = (uintptr_t)state % 16 == 0 && c.Dv % 4 == 0;
+  const long long units = (long long)c.B * c.kv_heads;
+  // whole rows of the state (512 bytes) in one workgroup where there are enough of them to fill the device
+  const bool wide = units >= SPLIT_TARGET && c.Dv > 32;
+  const long long grid = units * (wide ? (c.Dv + 127) / 128 : (c.Dv + 31) / 32);
+  if (grid > 0x7fffffffLL) return fail(MADE_ERR_ARG, "%s: B=%d, heads=%d are more than one launch takes", who, c.B, c.kv_heads);
+  hipStream_t s = (hipStream_t)stream;
+#define JM_STEP(T, COLS) hipLaunchKernelGGL((linattn_step_kernel<T, COLS>), dim3((unsigned)grid), dim3(256), 0, s, a)
+  if (c.dtype == MADE_BF16) {
+    if (wide) JM_STEP(la_bf16, 128);
+    else JM_STEP(la_bf16, 32);
+  } else {
+    if (wide) JM_STEP(float, 128);
+    else JM_STEP(float, 32);
+  }
+#undef JM_STEP
+  HIP_TRY(hipGetLastError());
+  return MADE_OK;
+}

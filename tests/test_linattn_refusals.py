@@ -1,0 +1,81 @@
+"""What the linear-attention entry points refuse, before any device work (no GPU needed)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2002_03629_amd import binding as B
+
+P = C.c_void_p(4096)       # a pointer that is never followed
+
+
+def config(**kw):
+    base = dict(B=2, T=8, heads=4, kv_heads=2, Dk=16, Dv=16, dtype=B.MADE_BF16, scale=1.0, ld_q=0, ld_k=0, ld_v=0, ld_o=0, offsets=None)
+    base.update(kw)
+    return B.linattn_config(*base.values())
+
+
+def calls(cfg, q=P, ws=None, ws_bytes=0, ds_in=None, ds_out=None):
+    L, n = B.lib(), None
+    c = C.byref(cfg) if cfg is not None else None
+    yield L.linattn_forward(c, q, P, P, P, n, P, n, ws, ws_bytes, n)
+    yield L.linattn_backward(c, q, P, P, P, n, P, ds_out, P, P, P, ds_in, ws, ws_bytes, n)
+
+
+BAD = [dict(B=-1), dict(Dk=0), dict(Dv=129), dict(heads=3), dict(kv_heads=0), dict(heads=0), dict(dtype=2), dict(scale=float("nan")),
+       dict(scale=float("inf")), dict(ld_q=63), dict(ld_k=31), dict(ld_v=1), dict(ld_o=-5), dict(ld_q=1 << 24), dict(heads=1 << 20)]
+
+
+@pytest.mark.parametrize("bad", BAD + [dict(T=-1)], ids=str)
+def test_bad_sizes(bad):
+    for code in calls(config(**bad)):
+        assert code == B.MADE_ERR_ARG
+        assert "linattn" in B.made_last_error()
+    out = C.c_int64()
+    assert B.lib().linattn_workspace_bytes(C.byref(config(**bad)), 0, C.byref(out)) == B.MADE_ERR_ARG
+
+
+@pytest.mark.parametrize("bad", BAD, ids=str)
+def test_bad_sizes_of_a_step(bad):
+    assert B.lib().linattn_step(C.byref(config(**bad)), P, P, P, P, P, 2, None, P, None) == B.MADE_ERR_ARG
+
+
+def test_null_arguments_and_workspaces():
+    assert all(code == B.MADE_ERR_ARG for code in calls(None))
+    assert all(code == B.MADE_ERR_ARG for code in calls(config(), q=None))
+    assert all(code == B.MADE_ERR_ARG for code in calls(config(), ws=C.c_void_p(4097), ws_bytes=1 << 20))
+    L = B.lib()
+    assert L.linattn_workspace_bytes(C.byref(config()), 0, None) == B.MADE_ERR_ARG
+    assert list(calls(config(), ds_in=P, ds_out=P))[1] == B.MADE_ERR_ARG and "d_state" in B.made_last_error()
+    assert L.linattn_step(C.byref(config()), P, P, P, P, None, 2, None, P, None) == B.MADE_ERR_ARG
+    assert L.linattn_step(C.byref(config()), P, P, P, P, P, 1, None, P, None) == B.MADE_ERR_ARG      # fewer places than rows
+    assert L.linattn_step(C.byref(config()), P, P, P, P, P, -1, P, P, None) == B.MADE_ERR_ARG
+
+
+def test_an_empty_batch_needs_no_pointers():
+    L = B.lib()
+    c = C.byref(config(B=0))
+    assert L.linattn_forward(c, None, None, None, None, None, None, None, None, 0, None) == B.MADE_OK
+    assert L.linattn_backward(c, *[None] * 12, 0, None) == B.MADE_OK
+    assert L.linattn_step(c, None, None, None, None, None, 0, None, None, None) == B.MADE_OK
+
+
+def test_workspace_sizes():
+    one = B.linattn_workspace_bytes(1, 64, 4, 2, 16, 16, torch.bfloat16)
+    assert one == 0                                            # one block: nothing to cut
+    long_ = B.linattn_workspace_bytes(1, 30000, 4, 2, 16, 16, torch.bfloat16)
+    assert long_ > 0 and long_ % (2 * 16 * 16 * 4) == 0
+    assert B.linattn_workspace_bytes(1, 30000, 4, 2, 16, 16, torch.bfloat16, backward=True) > 0
+    many = B.linattn_workspace_bytes(4096, 200, 8, 8, 128, 128, torch.bfloat16)
+    assert many == 0                                           # the sequences alone fill the device
+    with pytest.raises(B.MadeError):
+        B.linattn_workspace_bytes(1, 64, 3, 2, 16, 16, torch.bfloat16)
+
+
+def test_the_binding_refuses_tensors_of_the_host():
+    x = torch.zeros(2, 8, 4, 16, dtype=torch.bfloat16)
+    d = torch.zeros(4)
+    with pytest.raises(ValueError, match="GPU"):
+        B.linattn_forward(x, x, x, d, None, None, 2, 8, 4, 4, 16, 16, 1.0, x)
+    with pytest.raises(ValueError):
+        B.linattn_forward(x.half(), x, x, d, None, None, 2, 8, 4, 4, 16, 16, 1.0, x)
