@@ -71,48 +71,56 @@ Split choose(const linattn_config& c, int roles) {
 
 long long state_floats(const linattn_config& c, const Split& s) { return s.on ? (long long)s.slots * c.kv_heads * c.Dk * c.Dv : 0; }
 
-LinattnView view(const void* p, int64_t ld, int heads, int dim, int dtype) {
-  const int size = dtype == MADE_BF16 ? 2 : 4;
+LinattnView view(const void* p, int64_t ld, int heads, int dim) {
   LinattnView v;
   v.p = const_cast<void*>(p);
   v.ld = ld ? ld : (int64_t)heads * dim;
   v.dim = dim;
-  v.vec = (uintptr_t)p % 16 == 0 && v.ld * size % 16 == 0 && dim * size % 16 == 0;
   return v;
+}
+
+// Rows of 16-byte pieces: the base, the row stride and the width are multiples of 16 bytes.
+bool pieces(const LinattnView& v, int dtype) {
+  const int size = dtype == MADE_BF16 ? 2 : 4;
+  return !v.p || ((uintptr_t)v.p % 16 == 0 && v.ld * size % 16 == 0 && v.dim * size % 16 == 0);
 }
 
 int tiles(int d) { return d <= 32 ? 1 : d <= 64 ? 2 : 4; }
 
-template <typename T, int KT, int VT>
-void launch_walk(const LinattnArgs& a, bool out, hipStream_t s) {
+template <typename T, int KT, int VT, bool OUT, bool VEC>
+void launch_walk(const LinattnArgs& a, hipStream_t s) {
   const long long units = (long long)a.slots * a.kv_heads;
-  const dim3 grid((unsigned)((units + 7) / 8 * 8 * a.roles));
-  if (out) hipLaunchKernelGGL((linattn_walk_kernel<T, KT, VT, true>), grid, dim3(64 * VT), 0, s, a);
-  else hipLaunchKernelGGL((linattn_walk_kernel<T, KT, VT, false>), grid, dim3(64 * VT), 0, s, a);
+  hipLaunchKernelGGL((linattn_walk_kernel<T, KT, VT, OUT, VEC>), dim3((unsigned)((units + 7) / 8 * 8 * a.roles)), dim3(64 * VT), 0, s, a);
 }
 
-template <typename T, int KT>
-void launch_walk(int vt, const LinattnArgs& a, bool out, hipStream_t s) {
-  switch (vt) {
-    case 1: return launch_walk<T, KT, 1>(a, out, s);
-    case 2: return launch_walk<T, KT, 2>(a, out, s);
-    default: return launch_walk<T, KT, 4>(a, out, s);
-  }
-}
-
-template <typename T>
-void launch_walk(int kt, int vt, const LinattnArgs& a, bool out, hipStream_t s) {
-  switch (kt) {
-    case 1: return launch_walk<T, 1>(vt, a, out, s);
-    case 2: return launch_walk<T, 2>(vt, a, out, s);
-    default: return launch_walk<T, 4>(vt, a, out, s);
+template <typename T, bool OUT>
+void launch_walk(const LinattnArgs& a, bool vec, hipStream_t s) {
+  const int kt = tiles(a.role[0].dk), vt = tiles(a.role[0].dv);
+  // (operands that are fetched element by element: the square shapes do for all)
+  switch (vec ? 10 * kt + vt : std::max(kt, vt)) {
+    case 11: return launch_walk<T, 1, 1, OUT, true>(a, s);
+    case 12: return launch_walk<T, 1, 2, OUT, true>(a, s);
+    case 14: return launch_walk<T, 1, 4, OUT, true>(a, s);
+    case 21: return launch_walk<T, 2, 1, OUT, true>(a, s);
+    case 22: return launch_walk<T, 2, 2, OUT, true>(a, s);
+    case 24: return launch_walk<T, 2, 4, OUT, true>(a, s);
+    case 41: return launch_walk<T, 4, 1, OUT, true>(a, s);
+    case 42: return launch_walk<T, 4, 2, OUT, true>(a, s);
+    case 44: return launch_walk<T, 4, 4, OUT, true>(a, s);
+    case 1: return launch_walk<T, 1, 1, OUT, false>(a, s);
+    case 2: return launch_walk<T, 2, 2, OUT, false>(a, s);
+    default: return launch_walk<T, 4, 4, OUT, false>(a, s);
   }
 }
 
 void launch_walk(int dtype, const LinattnArgs& a, bool out, hipStream_t s) {
-  const int kt = tiles(a.role[0].dk), vt = tiles(a.role[0].dv);
-  if (dtype == MADE_BF16) launch_walk<la_bf16>(kt, vt, a, out, s);
-  else launch_walk<float>(kt, vt, a, out, s);
+  bool vec = true;
+  for (int i = 0; i < a.roles; ++i) {
+    const LinattnRole& r = a.role[i];
+    vec = vec && pieces(r.k, dtype) && pieces(r.v, dtype) && (!out || (pieces(r.q, dtype) && pieces(r.o, dtype)));
+  }
+  if (dtype == MADE_BF16) out ? launch_walk<la_bf16, true>(a, vec, s) : launch_walk<la_bf16, false>(a, vec, s);
+  else out ? launch_walk<float, true>(a, vec, s) : launch_walk<float, false>(a, vec, s);
 }
 
 void launch_join(const LinattnArgs& a, hipStream_t s) {
@@ -175,10 +183,10 @@ extern "C" int linattn_forward(const linattn_config* cfg, const void* q, const v
   LinattnArgs a = common(c, log_decay, split);
   a.roles = 1;
   LinattnRole& r = a.role[0];
-  r.q = view(q, c.ld_q, c.heads, c.Dk, c.dtype);
-  r.k = view(k, c.ld_k, c.kv_heads, c.Dk, c.dtype);
-  r.v = view(v, c.ld_v, c.kv_heads, c.Dv, c.dtype);
-  r.o = view(o, c.ld_o, c.heads, c.Dv, c.dtype);
+  r.q = view(q, c.ld_q, c.heads, c.Dk);
+  r.k = view(k, c.ld_k, c.kv_heads, c.Dk);
+  r.v = view(v, c.ld_v, c.kv_heads, c.Dv);
+  r.o = view(o, c.ld_o, c.heads, c.Dv);
   r.start = state_in;
   r.end = state_out;
   r.seg = split.on ? (float*)workspace : nullptr;
@@ -188,7 +196,7 @@ extern "C" int linattn_forward(const linattn_config* cfg, const void* q, const v
   r.st_c = 1;
   r.gq = c.heads / c.kv_heads;
   r.gk = 1;
-  r.parts = state_out ? 3 : 1;
+  r.parts = state_out ? 3 : 2;
   r.p_scale = r.i_scale = c.scale;
   r.s_scale = 1.0f;
   if (split.on) {
@@ -214,8 +222,8 @@ extern "C" int linattn_backward(const linattn_config* cfg, const void* q, const 
   TRY(check_grid(who, c, split, 3));
   hipStream_t s = (hipStream_t)stream;
   const int G = c.heads / c.kv_heads;
-  const LinattnView vq = view(q, c.ld_q, c.heads, c.Dk, c.dtype), vk = view(k, c.ld_k, c.kv_heads, c.Dk, c.dtype),
-                    vv = view(v, c.ld_v, c.kv_heads, c.Dv, c.dtype), vdo = view(d_o, c.ld_o, c.heads, c.Dv, c.dtype);
+  const LinattnView vq = view(q, c.ld_q, c.heads, c.Dk), vk = view(k, c.ld_k, c.kv_heads, c.Dk),
+                    vv = view(v, c.ld_v, c.kv_heads, c.Dv), vdo = view(d_o, c.ld_o, c.heads, c.Dv);
   float* seg_s = split.on ? (float*)workspace : nullptr;
   float* seg_r = split.on ? seg_s + state_floats(c, split) : nullptr;
   LinattnRole S, R;                                   // the states forward, and their gradients back in time
@@ -229,20 +237,20 @@ extern "C" int linattn_backward(const linattn_config* cfg, const void* q, const 
   S.st_r = c.Dv;
   S.st_c = 1;
   S.gq = S.gk = 1;
-  S.parts = 1;
+  S.parts = 2;
   S.p_scale = S.i_scale = c.scale;
   S.s_scale = 1.0f;
   R = S;
   R.q = vk;                                           // (as the role of dv)
   R.k = vq;
   R.v = vdo;
-  R.o = view(dv, c.ld_v, c.kv_heads, c.Dv, c.dtype);
+  R.o = view(dv, c.ld_v, c.kv_heads, c.Dv);
   R.start = d_state_out;
   R.end = d_state_in;
   R.seg = seg_r;
   R.gk = G;
   R.back = 1;
-  R.parts = d_state_in ? 3 : 1;
+  R.parts = d_state_in ? 3 : 2;
   R.i_scale = 1.0f;
   R.s_scale = c.scale;
   LinattnArgs a = common(c, log_decay, split);
@@ -257,14 +265,14 @@ extern "C" int linattn_backward(const linattn_config* cfg, const void* q, const 
   Q.q = vdo;
   Q.k = vv;
   Q.v = vk;
-  Q.o = view(dq, c.ld_q, c.heads, c.Dk, c.dtype);
+  Q.o = view(dq, c.ld_q, c.heads, c.Dk);
   Q.gq = G;
   K.q = vv;
   K.k = vdo;
   K.v = vq;
-  K.o = view(dk, c.ld_k, c.kv_heads, c.Dk, c.dtype);
+  K.o = view(dk, c.ld_k, c.kv_heads, c.Dk);
   K.end = nullptr;
-  K.parts = 1;
+  K.parts = 2;
   Q.dk = K.dk = c.Dv;
   Q.dv = K.dv = c.Dk;
   Q.st_r = K.st_r = 1;
@@ -295,10 +303,10 @@ extern "C" int linattn_step(const linattn_config* cfg, const void* q, const void
   if (c.B == 0) return MADE_OK;
   if (!q || !k || !v || !log_decay || !state || !o) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
   LinattnStepArgs a;
-  a.q = view(q, c.ld_q, c.heads, c.Dk, c.dtype);
-  a.k = view(k, c.ld_k, c.kv_heads, c.Dk, c.dtype);
-  a.v = view(v, c.ld_v, c.kv_heads, c.Dv, c.dtype);
-  a.o = view(o, c.ld_o, c.heads, c.Dv, c.dtype);
+  a.q = view(q, c.ld_q, c.heads, c.Dk);
+  a.k = view(k, c.ld_k, c.kv_heads, c.Dk);
+  a.v = view(v, c.ld_v, c.kv_heads, c.Dv);
+  a.o = view(o, c.ld_o, c.heads, c.Dv);
   a.log_decay = log_decay;
   a.state = state;
   a.slots = slots;

@@ -23,6 +23,8 @@ namespace jm {
 
 typedef uint16_t la_bf16;
 typedef __attribute__((ext_vector_type(4))) uint32_t la_u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t la_u32x2;
+typedef __attribute__((ext_vector_type(4))) float la_f32x4;
 typedef __attribute__((ext_vector_type(8))) __bf16 la_bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 la_bf16x4;
 typedef __attribute__((ext_vector_type(8))) float la_f32x8;
@@ -36,7 +38,6 @@ struct LinattnView {
   void* p;
   long long ld;
   int dim;
-  int vec;      // 1: 16-byte pieces of a row are aligned and whole (base, ld and dim are multiples of 16 bytes)
 };
 
 struct LinattnRole {
@@ -62,7 +63,11 @@ struct LinattnArgs {
   int slots;            // segments in all (packed: an upper bound)
 };
 
-__device__ __forceinline__ float la_pow(float g2, int n) { return n == 0 ? 1.0f : exp2f(g2 * (float)n); }   // lambda^n
+// lambda^n, g2 = log2 lambda (the hardware's exponential is within 1 ulp; below 2^-126 it is zero)
+__device__ __forceinline__ float la_pow(float g2, int n) {
+  const float x = __builtin_amdgcn_exp2f(g2 * (float)n);
+  return n == 0 ? 1.0f : x;
+}
 
 // ------------------------------------------------------------------------------------------------------------------
 // segments
@@ -152,8 +157,22 @@ struct LaShape<float> {
   static constexpr int C = 32;
 };
 
+// Memory is reached through buffer descriptors: a lane whose element does not exist gets an offset past the end, reads zero
+// and writes nothing, without a branch.  An offset is a lane's part, below 2^30 bytes or LA_NOWHERE, and a scalar part.
+constexpr unsigned LA_NOWHERE = 0x80000000u;
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t la_buffer(const void* p) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00027000);
+}
+
+// The C rows of a block as they lie in memory: position p of the walk is row p (forward) or C - 1 - p (back) from `base`.
+template <typename T>
+__device__ __forceinline__ const T* la_block(const LinattnView& x, long long first, int back, int head) {
+  return (const T*)x.p + (back ? first - (LaShape<T>::C - 1) : first) * x.ld + (long long)head * x.dim;
+}
+
 // A thread's share of a block of an operand whose rows come in 16-byte pieces: groups of 4 consecutive rows x 1 piece,
-// group tid + i NT.  A piece's address is one register's offset from a scalar base of its own.
+// group tid + i NT.
 template <typename T, int TILES, int NT>
 struct LaStage {
   static constexpr int C = LaShape<T>::C;
@@ -167,21 +186,20 @@ struct LaStage {
   static __device__ __forceinline__ int piece() { return threadIdx.x % U; }
   static __device__ __forceinline__ int group() { return threadIdx.x / U; }
 
-  // rows at positions 0 .. n-1 of the block: row `first + p` (forward) or `first - p` (back); beyond n and dim: zeros
+  // rows at positions 0 .. n-1 of the block; beyond n and dim: zeros
   __device__ __forceinline__ void load(const LinattnView& x, long long first, int back, int n, int head) {
-    const int ld = (int)x.ld * (int)sizeof(T);                // (at most 2^25 bytes: the host checks)
-    const unsigned off = (unsigned)((back ? NTG - 1 - group() : group()) * 4) * (unsigned)ld + piece() * 16;
-    const char* base = (const char*)x.p + ((back ? first - 4 * (NTG - 1) : first) * x.ld + (long long)head * x.dim) * (long long)sizeof(T);
+    const __amdgpu_buffer_rsrc_t buf = la_buffer(la_block<T>(x, first, back, head));
+    const unsigned ld = (unsigned)x.ld * (unsigned)sizeof(T);                // (at most 2^25 bytes: the host checks)
+    const int t0 = group(), t0_row = back ? C / 4 - 1 - (PER - 1) * NTG - t0 : t0;
+    const unsigned off = (unsigned)(4 * t0_row) * ld + piece() * 16;
     const bool in_row = piece() * PIECE < x.dim;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const long long step = (long long)(4 * i * NTG + e) * ld;
-        const char* src = back ? base - step : base + step;
-        la_u32x4 w = {0, 0, 0, 0};
-        if (in_row && 4 * (group() + i * NTG) + e < n) w = *(const la_u32x4*)(src + off);
-        r[i][e] = w;
+        const unsigned rows = back ? 4 * (PER - 1 - i) * NTG + 3 - e : 4 * i * NTG + e;
+        const bool there = in_row && 4 * (t0 + i * NTG) + e < n;
+        r[i][e] = __builtin_amdgcn_raw_buffer_load_b128(buf, there ? off : LA_NOWHERE, __builtin_amdgcn_readfirstlane(rows * ld), 0);
       }
   }
 };
@@ -248,14 +266,16 @@ __device__ __forceinline__ void la_put_columns(const LaStage<la_bf16, TILES, NT>
   for (int i = 0; i < S::PER; ++i) {
     const int tg = t0 + i * S::NTG;
     if (tg < 16) {
+      // (la_swizzle(8 u + dd) = la_swizzle(8 u) ^ dd / 2: four addresses and fixed distances from them)
+      unsigned char* column = dst + 8 * u * 128 + la_half(tg) * 8;
+      const int unit = la_unit(tg) ^ la_swizzle(8 * u);
 #pragma unroll
       for (int dd = 0; dd < 8; ++dd) {
         const uint32_t sel = dd & 1 ? 0x07060302u : 0x05040100u;
-        const int d = 8 * u + dd;
         uint2 o;
         o.x = __builtin_amdgcn_perm(st.r[i][1][dd / 2], st.r[i][0][dd / 2], sel);
         o.y = __builtin_amdgcn_perm(st.r[i][3][dd / 2], st.r[i][2][dd / 2], sel);
-        *(uint2*)(dst + d * 128 + (la_unit(tg) ^ la_swizzle(d)) * 16 + la_half(tg) * 8) = o;
+        *(uint2*)(column + ((unit ^ (dd / 2)) * 16) + dd * 128) = o;
       }
     }
   }
@@ -306,10 +326,13 @@ __device__ __forceinline__ void la_fetch_rows(const LinattnView& x, long long fi
   }
 }
 
+// fp32 values as two bf16 parts, x = hi + lo + O(2^-17 x)
 __device__ __forceinline__ la_bf16x8 la_round(la_f32x8 x) { return __builtin_convertvector(x, la_bf16x8); }
+__device__ __forceinline__ la_bf16x8 la_rest(la_f32x8 x, la_bf16x8 hi) { return la_round(x - __builtin_convertvector(hi, la_f32x8)); }
 
 // OUT = true: the walk with outputs.  OUT = false: only the state a segment adds, from zero, into the workspace.
-template <typename T, int KT, int VT, bool OUT>
+// VEC: every operand's rows come in 16-byte pieces (else none is taken to).
+template <typename T, int KT, int VT, bool OUT, bool VEC>
 __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(LinattnArgs a) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int C = LaShape<T>::C, IT = C / 32, NT = 64 * VT;
@@ -324,6 +347,12 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
   const int head = unit % a.kv_heads;
   LinattnSegment s;
   if (!la_find(a, unit / a.kv_heads, s)) return;
+  // (the same in every lane: they form addresses that are scalars)
+  s.b = __builtin_amdgcn_readfirstlane(s.b);
+  s.index = __builtin_amdgcn_readfirstlane(s.index);
+  s.count = __builtin_amdgcn_readfirstlane(s.count);
+  s.row0 = __builtin_amdgcn_readfirstlane(s.row0);
+  s.len = __builtin_amdgcn_readfirstlane(s.len);
   if (!OUT && s.index == s.count - 1) return;    // (nothing follows the last segment)
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -338,18 +367,18 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
   // ---- state: element e = 4 jj + i of tile kt is (key 32 kt + 8 jj + 4 hh + i, value 32 wave + cl)
   la_f32x16 S[KT];
   const int col = 32 * wave + cl;
+  unsigned state_off = (unsigned)(4 * hh * R.st_r + col * R.st_c) * 4;
+  const long long seg_at = ((long long)(unit / a.kv_heads) * a.kv_heads + head) * R.dk * R.dv;
   {
-    const float* src = nullptr;
-    if (OUT) {
-      if (R.seg && s.count > 1) src = R.seg + ((long long)(unit / a.kv_heads) * a.kv_heads + head) * R.dk * R.dv;
-      else if (R.start) src = R.start + state_at;
-    }
+    const float* src = !OUT ? nullptr : R.seg && s.count > 1 ? R.seg + seg_at : R.start ? R.start + state_at : nullptr;
+    const __amdgpu_buffer_rsrc_t buf = la_buffer(src);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int key = 32 * kt + 8 * (e / 4) + 4 * hh + e % 4;
-        S[kt][e] = src && key < R.dk && col < R.dv ? src[(long long)key * R.st_r + (long long)col * R.st_c] : 0.0f;
+        const int key = 32 * kt + 8 * (e / 4) + e % 4;
+        const bool there = src && key + 4 * hh < R.dk && col < R.dv;
+        S[kt][e] = OUT ? __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buf, there ? state_off : LA_NOWHERE, key * R.st_r * 4, 0)) : 0.0f;
       }
   }
 
@@ -359,7 +388,8 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int j = 8 * (e / 4) + 4 * hh + e % 4;
-      diag[e] = j <= cl ? R.p_scale * la_pow(g2, cl - j) : 0.0f;
+      const float x = R.p_scale * la_pow(g2, max(cl - j, 0));
+      diag[e] = j <= cl ? x : 0.0f;
     }
 #pragma unroll
     for (int it = 0; it < IT; ++it) row_in[it] = R.i_scale * la_pow(g2, 32 * it + cl + 1 - late);
@@ -377,10 +407,10 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
   auto request = [&](int p, int st) {
     const long long row = R.back ? first - p : first + p;
     const int n = min(C, p1 - p);
-    if (OUT && R.q.vec && (R.gq > 1 || st == 0)) qs.load(R.q, row, R.back, n, q_head(st));
-    if (R.gk > 1 || st == 0) {
-      if (R.k.vec) ks.load(R.k, row, R.back, n, k_head(st));
-      if (R.v.vec) vs.load(R.v, row, R.back, n, k_head(st));
+    if (OUT && VEC && (R.gq > 1 || st == 0)) qs.load(R.q, row, R.back, n, q_head(st));
+    if (VEC && (R.gk > 1 || st == 0)) {
+      ks.load(R.k, row, R.back, n, k_head(st));
+      vs.load(R.v, row, R.back, n, k_head(st));
     }
   };
   if (p0 < p1) request(p0, 0);
@@ -394,24 +424,24 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
       __syncthreads();                       // every wave has read the block before
       const long long row = R.back ? first - p : first + p;
       if (OUT && new_q) {
-        if (R.q.vec) la_put_rows(qs, lds.q, lds.PITCH);
+        if (VEC) la_put_rows(qs, lds.q, lds.PITCH);
         else la_fetch_rows<KT, NT>(R.q, row, R.back, n, q_head(st), lds.q, lds.PITCH);
       }
       if (new_kv) {
         if constexpr (F32) {
-          if (R.k.vec) la_put_rows(ks, lds.k, lds.PITCH);
+          if (VEC) la_put_rows(ks, lds.k, lds.PITCH);
           else la_fetch_rows<KT, NT>(R.k, row, R.back, n, k_head(st), lds.k, lds.PITCH);
-          if (R.v.vec) la_put_rows(vs, lds.v, lds.VPITCH);
+          if (VEC) la_put_rows(vs, lds.v, lds.VPITCH);
           else la_fetch_rows<VT, NT>(R.v, row, R.back, n, k_head(st), lds.v, lds.VPITCH);
         } else {
-          if (R.k.vec) {
+          if (VEC) {
             if (OUT) la_put_rows(ks, lds.k, lds.PITCH);
             la_put_columns(ks, lds.kt);
           } else {
             if (OUT) la_fetch_rows<KT, NT>(R.k, row, R.back, n, k_head(st), lds.k, lds.PITCH);
             la_fetch_columns<KT, NT>(R.k, row, R.back, n, k_head(st), lds.kt);
           }
-          if (R.v.vec) la_put_columns(vs, lds.vt);
+          if (VEC) la_put_columns(vs, lds.vt);
           else la_fetch_columns<VT, NT>(R.v, row, R.back, n, k_head(st), lds.vt);
         }
         if (threadIdx.x < C) lds.weight[threadIdx.x] = R.s_scale * la_pow(g2, max(0, n - 1 + late - (int)threadIdx.x));
@@ -421,10 +451,14 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
       __syncthreads();
 
       if constexpr (!F32) {
+        // (la_swizzle(32 n + c) = la_swizzle(c) ^ 2 n: unit 2 mb + hh of column 32 kt + cl lies where mb ^ kt says)
         const unsigned char* kt_ = lds.kt + cl * 128;
         const unsigned char* vt_ = lds.vt + (32 * wave + cl) * 128;
-        const int vsw = la_swizzle(32 * wave + cl);
-        auto v_frag = [&](int mb) { return __builtin_bit_cast(la_bf16x8, *(const uint4*)(vt_ + ((2 * mb + hh) ^ vsw) * 16)); };
+        const int ksw = (hh ^ la_swizzle(cl)) * 16, vsw = (hh ^ la_swizzle(32 * wave + cl)) * 16;
+        auto v_frag = [&](int mb) { return __builtin_bit_cast(la_bf16x8, *(const uint4*)(vt_ + (vsw ^ 32 * mb))); };
+        auto kt_frag = [&](int kt, int mb) {
+          return __builtin_bit_cast(la_bf16x8, *(const uint4*)(kt_ + (ksw ^ 32 * (mb ^ kt)) + kt * 32 * 128));
+        };
         if (OUT) {
           const unsigned char* q_ = lds.q + cl * lds.PITCH + hh * 16;
           const unsigned char* k_ = lds.k + cl * lds.PITCH + hh * 16;
@@ -443,10 +477,13 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
                 la_f32x8 x;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = S[kt][8 * mm + e];
-                const la_bf16x8 sf = la_round(x);
+                const la_bf16x8 hi = la_round(x), lo = la_rest(x, hi);
 #pragma unroll
-                for (int it = 0; it < IT; ++it)
-                  O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(sf, q_frag(it, 2 * kt + mm), O[it], 0, 0, 0);
+                for (int it = 0; it < IT; ++it) {
+                  const la_bf16x8 qf = q_frag(it, 2 * kt + mm);
+                  O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, qf, O[it], 0, 0, 0);
+                  O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, qf, O[it], 0, 0, 0);
+                }
               }
 #pragma unroll
             for (int it = 0; it < IT; ++it)
@@ -470,12 +507,19 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
               la_f32x8 x;
 #pragma unroll
               for (int e = 0; e < 8; ++e) x[e] = P[8 * mm + e];
-              O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(2 * jt + mm), la_round(x), O[it], 0, 0, 0);
+              const la_bf16x8 hi = la_round(x), vf = v_frag(2 * jt + mm);
+              O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, hi, O[it], 0, 0, 0);
+              O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, la_rest(x, hi), O[it], 0, 0, 0);
             }
           };
+          // (an operand is read again rather than kept from one product to the next: 64 registers would hold q alone)
+          asm volatile("" ::: "memory");
           tile(0, 0);
+          asm volatile("" ::: "memory");
           tile(0, 1);
+          asm volatile("" ::: "memory");
           tile(1, 1);
+          asm volatile("" ::: "memory");
         }
         // S = lambda^n S + K^T V'
         if (R.gk > 1 ? st == 0 : last) {
@@ -494,9 +538,7 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
               const la_bf16x8 h = la_round(x);
 #pragma unroll
               for (int kt = 0; kt < KT; ++kt) {
-                const int d = 32 * kt + cl;
-                const la_bf16x8 kf = __builtin_bit_cast(la_bf16x8, *(const uint4*)(kt_ + kt * 32 * 128 + ((2 * mb + hh) ^ la_swizzle(d)) * 16));
-                S[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, h, S[kt], 0, 0, 0);
+                S[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kt_frag(kt, mb), h, S[kt], 0, 0, 0);
               }
               x -= __builtin_convertvector(h, la_f32x8);
             }
@@ -560,34 +602,26 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
 
       if (OUT && (R.gq > 1 || last)) {
         // element e = 4 jj + i of tile it is (value 32 wave + 8 jj + 4 hh + i, step 32 it + cl)
-        T* out = (T*)R.o.p + (long long)(head * R.gq + (R.gq > 1 ? st : 0)) * R.o.dim;
+        const __amdgpu_buffer_rsrc_t buf = la_buffer(la_block<T>(R.o, row, R.back, q_head(st)));
+        const unsigned ld = (unsigned)R.o.ld;
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
           const int pos = 32 * it + cl;
-          if (pos < n) {
-            T* dst = out + (R.back ? first - p - pos : first + p + pos) * R.o.ld;
+          const unsigned off = ((unsigned)(R.back ? C - 1 - pos : pos) * ld + 32 * wave + 4 * hh) * (unsigned)sizeof(T);
 #pragma unroll
-            for (int jj = 0; jj < 4; ++jj) {
-              const int c0 = 32 * wave + 8 * jj + 4 * hh;
-              if constexpr (F32) {
-                if (R.o.vec) {
-                  if (c0 < R.dv) *(float4*)(dst + c0) = make_float4(O[it][4 * jj], O[it][4 * jj + 1], O[it][4 * jj + 2], O[it][4 * jj + 3]);
-                } else {
+          for (int jj = 0; jj < 4; ++jj) {
+            const int c0 = 32 * wave + 8 * jj + 4 * hh;
+            const la_f32x4 y = {O[it][4 * jj], O[it][4 * jj + 1], O[it][4 * jj + 2], O[it][4 * jj + 3]};
+            if (VEC) {
+              const unsigned at = pos < n && c0 < R.dv ? off : LA_NOWHERE;
+              if constexpr (F32) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(la_u32x4, y), buf, at, 32 * jj, 0);
+              else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(la_u32x2, __builtin_convertvector(y, la_bf16x4)), buf, at, 16 * jj, 0);
+            } else {
 #pragma unroll
-                  for (int i = 0; i < 4; ++i)
-                    if (c0 + i < R.dv) dst[c0 + i] = O[it][4 * jj + i];
-                }
-              } else {
-                const la_bf16x4 h = {(__bf16)O[it][4 * jj], (__bf16)O[it][4 * jj + 1], (__bf16)O[it][4 * jj + 2], (__bf16)O[it][4 * jj + 3]};
-                if (R.o.vec) {
-                  if (c0 < R.dv) *(la_bf16x4*)(dst + c0) = h;
-                } else {
-                  const uint2 w = __builtin_bit_cast(uint2, h);
-                  const la_bf16 t[4] = {(la_bf16)w.x, (la_bf16)(w.x >> 16), (la_bf16)w.y, (la_bf16)(w.y >> 16)};
-#pragma unroll
-                  for (int i = 0; i < 4; ++i)
-                    if (c0 + i < R.dv) dst[c0 + i] = t[i];
-                }
+              for (int i = 0; i < 4; ++i) {
+                const unsigned at = pos < n && c0 + i < R.dv ? off : LA_NOWHERE;
+                if constexpr (F32) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(y[i]), buf, at, 32 * jj + 4 * i, 0);
+                else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(short, (__bf16)y[i]), buf, at, 16 * jj + 2 * i, 0);
               }
             }
           }
@@ -596,16 +630,18 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
     }
   }
 
-  float* dst = nullptr;
-  if (!OUT) dst = R.seg + ((long long)(unit / a.kv_heads) * a.kv_heads + head) * R.dk * R.dv;
-  else if (R.end && s.index == s.count - 1) dst = R.end + state_at;
-  if (dst && col < R.dv) {
+  float* dst = !OUT ? R.seg + seg_at : R.end && s.index == s.count - 1 ? R.end + state_at : nullptr;
+  if (dst) {
+    const __amdgpu_buffer_rsrc_t buf = la_buffer(dst);
+    int key0 = 4 * hh, col0 = col;
+    asm volatile("" : "+v"(state_off), "+v"(key0), "+v"(col0));      // (formed again, not kept from the loads)
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int key = 32 * kt + 8 * (e / 4) + 4 * hh + e % 4;
-        if (key < R.dk) dst[(long long)key * R.st_r + (long long)col * R.st_c] = S[kt][e];
+        const int key = 32 * kt + 8 * (e / 4) + e % 4;
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[kt][e]), buf, key + key0 < R.dk && col0 < R.dv ? state_off : LA_NOWHERE,
+                                              key * R.st_r * 4, 0);
       }
   }
 }
