@@ -55,10 +55,10 @@ Split choose(const linattn_config& c, int roles) {
   if (blocks <= 1) return whole;
   auto slots = [&](long long L) { return c.offsets ? blocks / L + seqs : (blocks + L - 1) / L * seqs; };
   auto rounds = [&](long long n) { return (double)std::max<long long>(1, (n * units + SPLIT_TARGET - 1) / SPLIT_TARGET); };
-  double best = rounds(seqs) * blocks;
+  double best = rounds(seqs) * (blocks + 2);
   long long best_l = blocks;
   for (long long L = 1; L < blocks; L = L < 8 ? L + 1 : L + L / 4) {
-    const double cost = rounds(slots(L)) * L * 1.5 + 8.0;
+    const double cost = rounds(slots(L)) * (1.5 * L + 5) + 0.3 * blocks / L + 8;
     if (cost < best) {
       best = cost;
       best_l = L;

@@ -223,7 +223,8 @@ struct LaLds<la_bf16, KT, VT, OUT> {
   __align__(16) unsigned char kt[KT * 32 * 128];
   __align__(16) unsigned char vt[VT * 32 * 128];
   __align__(16) float weight[64];      // lambda^(n-1+late-j) of step j of the block: what the block's end keeps of it
-  __align__(16) float across[32];      // lambda^(32-j): from step j of the block's first half to its middle
+  __align__(16) float fade[96];        // p_scale lambda^m at 31 + m, zeros before: the factor of a pair of steps m apart
+  __align__(16) unsigned char p[OUT ? 3 : 1][2][2][64 * 16];   // scores as operands: tile, half of its steps, part, lane
 };
 template <int KT, int VT, bool OUT>
 struct LaLds<float, KT, VT, OUT> {
@@ -232,6 +233,8 @@ struct LaLds<float, KT, VT, OUT> {
   __align__(16) float k[32 * PITCH];
   __align__(16) float v[32 * VPITCH];
   __align__(16) float weight[32];
+  __align__(16) float fade[64];
+  la_f32x4 p[OUT ? VT : 1][4][64];     // each wave's share of the scores' sums: quad of rows, lane
 };
 
 __device__ __forceinline__ int la_swizzle(int d) { return ((d >> 1) ^ (d >> 4)) & 7; }
@@ -382,38 +385,31 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
       }
   }
 
-  // ---- decay factors of a block's pairs: the diagonal tile's, lambda^(i-j) for j <= i (row j, column i), times p_scale
-  float diag[16], row_in[IT];
+  float row_in[IT];
   if (OUT) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int j = 8 * (e / 4) + 4 * hh + e % 4;
-      const float x = R.p_scale * la_pow(g2, max(cl - j, 0));
-      diag[e] = j <= cl ? x : 0.0f;
-    }
+    for (int i = threadIdx.x; i < C + 32; i += NT) lds.fade[i] = i < 31 ? 0.0f : R.p_scale * la_pow(g2, i - 31);
 #pragma unroll
     for (int it = 0; it < IT; ++it) row_in[it] = R.i_scale * la_pow(g2, 32 * it + cl + 1 - late);
-    if constexpr (!F32) {
-      if (threadIdx.x < 32) lds.across[threadIdx.x] = R.p_scale * la_pow(g2, 32 - (int)threadIdx.x);
-    }
   }
-  const float cross = la_pow(g2, cl);      // from the block's middle to step 32 + cl
 
   LaStage<T, KT, NT> qs, ks;
   LaStage<T, VT, NT> vs;
   const int stages = R.gq > R.gk ? R.gq : R.gk;
   const auto q_head = [&](int st) { return head * R.gq + (R.gq > 1 ? st : 0); };
   const auto k_head = [&](int st) { return head * R.gk + (R.gk > 1 ? st : 0); };
+  // The next block's pieces, always into the same registers: what a stage does not need is asked for from nowhere (a branch
+  // around the loads would have their results moved, and so waited for, where it ends).
   auto request = [&](int p, int st) {
     const long long row = R.back ? first - p : first + p;
-    const int n = min(C, p1 - p);
-    if (OUT && VEC && (R.gq > 1 || st == 0)) qs.load(R.q, row, R.back, n, q_head(st));
-    if (VEC && (R.gk > 1 || st == 0)) {
-      ks.load(R.k, row, R.back, n, k_head(st));
-      vs.load(R.v, row, R.back, n, k_head(st));
+    const int n = min(C, p1 - p);                                          // (none behind the last block)
+    if (OUT && VEC) qs.load(R.q, row, R.back, R.gq > 1 || st == 0 ? n : 0, q_head(st));
+    if (VEC) {
+      const int nk = R.gk > 1 || st == 0 ? n : 0;
+      ks.load(R.k, row, R.back, nk, k_head(st));
+      vs.load(R.v, row, R.back, nk, k_head(st));
     }
   };
-  if (p0 < p1) request(p0, 0);
+  request(p0, 0);
 
   la_f32x16 O[IT];
   for (int p = p0; p < p1; p += C) {
@@ -446,8 +442,7 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
         }
         if (threadIdx.x < C) lds.weight[threadIdx.x] = R.s_scale * la_pow(g2, max(0, n - 1 + late - (int)threadIdx.x));
       }
-      if (!last) request(p, st + 1);
-      else if (p + C < p1) request(p + C, 0);
+      request(last ? p + C : p, last ? 0 : st + 1);
       __syncthreads();
 
       if constexpr (!F32) {
@@ -464,12 +459,30 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
           const unsigned char* k_ = lds.k + cl * lds.PITCH + hh * 16;
           auto q_frag = [&](int it, int m) { return __builtin_bit_cast(la_bf16x8, *(const uint4*)(q_ + it * 32 * lds.PITCH + m * 32)); };
           auto k_frag = [&](int jt, int m) { return __builtin_bit_cast(la_bf16x8, *(const uint4*)(k_ + jt * 32 * lds.PITCH + m * 32)); };
+          // Scores of the tiles (steps jt, queries it), transposed, a tile to a wave: every wave needs them all, as operands
+          // in two parts, and gets them through LDS while its product with the state runs.
+#pragma unroll
+          for (int t = 0; t < 3; ++t) {
+            if (t % VT != wave) continue;
+            const int jt = t >> 1, it = (t + 1) >> 1;
+            la_f32x16 P = {};
+#pragma unroll
+            for (int m = 0; m < 2 * KT; ++m) P = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(jt, m), q_frag(it, m), P, 0, 0, 0);
+            const float* f = lds.fade + 31 + 32 * (it - jt) + cl - 4 * hh;
+#pragma unroll
+            for (int mm = 0; mm < 2; ++mm) {
+              la_f32x8 x;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] = P[8 * mm + e] * f[-(16 * mm + 8 * (e / 4) + e % 4)];
+              const la_bf16x8 hi = la_round(x);
+              *(la_bf16x8*)&lds.p[t][mm][0][lane * 16] = hi;
+              *(la_bf16x8*)&lds.p[t][mm][1][lane * 16] = la_rest(x, hi);
+            }
+          }
           if (new_q) {
             // O^T = S^T Q^T: the accumulator of the state is an operand as it lies
 #pragma unroll
-            for (int it = 0; it < IT; ++it)
-#pragma unroll
-              for (int e = 0; e < 16; ++e) O[it][e] = 0.0f;
+            for (int it = 0; it < IT; ++it) O[it] = la_f32x16{};
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -490,36 +503,18 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
 #pragma unroll
               for (int e = 0; e < 16; ++e) O[it][e] *= row_in[it];
           }
-          // scores of the tiles (steps jt, queries it), transposed; O^T += V^T P^T
-          auto tile = [&](int jt, int it) {
-            la_f32x16 P;
+          __syncthreads();
+          // O^T += V^T P^T
 #pragma unroll
-            for (int e = 0; e < 16; ++e) P[e] = 0.0f;
-#pragma unroll
-            for (int m = 0; m < 2 * KT; ++m) P = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(jt, m), q_frag(it, m), P, 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              if (jt == it) P[e] = diag[e] != 0.0f ? P[e] * diag[e] : 0.0f;
-              else P[e] *= lds.across[8 * (e / 4) + 4 * hh + e % 4] * cross;
-            }
+          for (int t = 0; t < 3; ++t) {
+            const int jt = t >> 1, it = (t + 1) >> 1;
 #pragma unroll
             for (int mm = 0; mm < 2; ++mm) {
-              la_f32x8 x;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = P[8 * mm + e];
-              const la_bf16x8 hi = la_round(x), vf = v_frag(2 * jt + mm);
-              O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, hi, O[it], 0, 0, 0);
-              O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, la_rest(x, hi), O[it], 0, 0, 0);
+              const la_bf16x8 vf = v_frag(2 * jt + mm);
+              O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, *(const la_bf16x8*)&lds.p[t][mm][0][lane * 16], O[it], 0, 0, 0);
+              O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, *(const la_bf16x8*)&lds.p[t][mm][1][lane * 16], O[it], 0, 0, 0);
             }
-          };
-          // (an operand is read again rather than kept from one product to the next: 64 registers would hold q alone)
-          asm volatile("" ::: "memory");
-          tile(0, 0);
-          asm volatile("" ::: "memory");
-          tile(0, 1);
-          asm volatile("" ::: "memory");
-          tile(1, 1);
-          asm volatile("" ::: "memory");
+          }
         }
         // S = lambda^n S + K^T V'
         if (R.gk > 1 ? st == 0 : last) {
@@ -549,9 +544,21 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
         if (OUT) {
           const float* q_ = lds.q + cl * lds.PITCH + 4 * hh;
           const float* k_ = lds.k + cl * lds.PITCH + 4 * hh;
-          if (new_q) {
+          // each wave takes its share of the scores' sum over the keys' width
+          la_f32x16 P = {};
 #pragma unroll
-            for (int e = 0; e < 16; ++e) O[0][e] = 0.0f;
+          for (int i = 0; i < 4 * KT / VT; ++i) {
+            const int m = wave + i * VT;
+            const float4 k4 = *(const float4*)(k_ + 8 * m), q4 = *(const float4*)(q_ + 8 * m);
+            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.x, q4.x, P, 0, 0, 0);
+            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.y, q4.y, P, 0, 0, 0);
+            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.z, q4.z, P, 0, 0, 0);
+            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.w, q4.w, P, 0, 0, 0);
+          }
+#pragma unroll
+          for (int jj = 0; jj < 4; ++jj) lds.p[wave][jj][lane] = la_f32x4{P[4 * jj], P[4 * jj + 1], P[4 * jj + 2], P[4 * jj + 3]};
+          if (new_q) {
+            O[0] = la_f32x16{};
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -565,19 +572,16 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
 #pragma unroll
             for (int e = 0; e < 16; ++e) O[0][e] *= row_in[0];
           }
-          la_f32x16 P;
+          __syncthreads();
+          const float* f = lds.fade + 31 + cl - 4 * hh;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) P[e] = 0.0f;
+          for (int jj = 0; jj < 4; ++jj) {
+            la_f32x4 x = lds.p[0][jj][lane];
 #pragma unroll
-          for (int m = 0; m < 4 * KT; ++m) {
-            const float4 k4 = *(const float4*)(k_ + 8 * m), q4 = *(const float4*)(q_ + 8 * m);
-            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.x, q4.x, P, 0, 0, 0);
-            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.y, q4.y, P, 0, 0, 0);
-            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.z, q4.z, P, 0, 0, 0);
-            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.w, q4.w, P, 0, 0, 0);
+            for (int w = 1; w < VT; ++w) x += lds.p[w][jj][lane];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) P[4 * jj + i] = x[i] * f[-(8 * jj + i)];
           }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) P[e] = diag[e] != 0.0f ? P[e] * diag[e] : 0.0f;
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             O[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_[(8 * (e / 4) + e % 4) * lds.VPITCH], P[e], O[0], 0, 0, 0);
