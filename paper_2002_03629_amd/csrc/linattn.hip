@@ -14,7 +14,7 @@ namespace {
 
 constexpr int SPLIT_TARGET = 512;      // workgroups that fill the device: two to a compute unit
 
-int block_rows(const linattn_config& c) { return c.dtype == MADE_BF16 ? LaShape<la_bf16>::C : LaShape<float>::C; }
+int block_rows(const linattn_config& c) { return c.dtype == MADE_BF16 ? LA_BF16_ROWS : LA_F32_ROWS; }
 
 int check(const char* who, const linattn_config* c, bool step) {
   if (!c) return fail(MADE_ERR_ARG, "%s: NULL config", who);
@@ -89,8 +89,9 @@ int tiles(int d) { return d <= 32 ? 1 : d <= 64 ? 2 : 4; }
 
 template <typename T, int KT, int VT, bool OUT, bool VEC>
 void launch_walk(const LinattnArgs& a, hipStream_t s) {
-  const long long units = (long long)a.slots * a.kv_heads;
-  hipLaunchKernelGGL((linattn_walk_kernel<T, KT, VT, OUT, VEC>), dim3((unsigned)((units + 7) / 8 * 8 * a.roles)), dim3(64 * VT), 0, s, a);
+  const dim3 grid((unsigned)(((long long)a.slots * a.kv_heads + 7) / 8 * 8 * a.roles));
+  if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((linattn_walk_bf16_kernel<KT, VT, OUT, VEC>), grid, dim3(128 * VT), 0, s, a);
+  else hipLaunchKernelGGL((linattn_walk_f32_kernel<KT, VT, OUT, VEC>), grid, dim3(64 * VT), 0, s, a);
 }
 
 template <typename T, bool OUT>

@@ -146,63 +146,48 @@ __device__ __forceinline__ int la_first_slot(const LinattnArgs& a, int b, int& l
 // ------------------------------------------------------------------------------------------------------------------
 // the walk
 // ------------------------------------------------------------------------------------------------------------------
-template <typename T>
-struct LaShape;
-template <>
-struct LaShape<la_bf16> {
-  static constexpr int C = 64;
-};
-template <>
-struct LaShape<float> {
-  static constexpr int C = 32;
-};
+constexpr int LA_BF16_ROWS = 64, LA_F32_ROWS = 32;      // steps of a block
 
 // Memory is reached through buffer descriptors: a lane whose element does not exist gets an offset past the end, reads zero
 // and writes nothing, without a branch.  An offset is a lane's part, below 2^30 bytes or LA_NOWHERE, and a scalar part.
 constexpr unsigned LA_NOWHERE = 0x80000000u;
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t la_buffer(const void* p) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00027000);
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t la_buffer(const void* p, int bytes = 0x7fffffff) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
 }
 
-// The C rows of a block as they lie in memory: position p of the walk is row p (forward) or C - 1 - p (back) from `base`.
+// n rows of an operand from the row of position 0 (`first`) on, in the order of the walk.  The descriptor begins at their
+// lowest row and ends behind their highest; position p is la_row(...) bytes from its begin: what lies behind the n rows falls
+// out of it, forward above its end, back below zero.
 template <typename T>
-__device__ __forceinline__ const T* la_block(const LinattnView& x, long long first, int back, int head) {
-  return (const T*)x.p + (back ? first - (LaShape<T>::C - 1) : first) * x.ld + (long long)head * x.dim;
+struct LaBlock {
+  __amdgpu_buffer_rsrc_t buf;
+  int ld;                   // bytes from row to row (at most 2^25: the host checks), negative back in time
+  unsigned at0;             // of position 0
+};
+template <typename T>
+__device__ __forceinline__ LaBlock<T> la_block(const LinattnView& x, long long first, int back, int n, int head) {
+  LaBlock<T> b;
+  const T* base = (const T*)x.p + (back ? first - (n - 1) : first) * x.ld + (long long)head * x.dim;
+  const int ld = (int)x.ld * (int)sizeof(T);
+  b.buf = la_buffer(base, __builtin_amdgcn_readfirstlane(n * ld));
+  b.ld = back ? -ld : ld;
+  b.at0 = back ? (unsigned)((n - 1) * ld) : 0u;
+  return b;
+}
+// A lane's part of an offset: position p, element d of the head; LA_NOWHERE for elements that do not exist.
+template <typename T>
+__device__ __forceinline__ unsigned la_lane(const LinattnView& x, int back, int p, int d) {
+  const int ld = (int)x.ld * (int)sizeof(T);
+  return d < x.dim ? (unsigned)((back ? -p : p) * ld + d * (int)sizeof(T)) : LA_NOWHERE;
 }
 
-// A thread's share of a block of an operand whose rows come in 16-byte pieces: groups of 4 consecutive rows x 1 piece,
-// group tid + i NT.
-template <typename T, int TILES, int NT>
-struct LaStage {
-  static constexpr int C = LaShape<T>::C;
-  static constexpr int PIECE = 16 / sizeof(T);
-  static constexpr int U = TILES * 32 / PIECE;                // pieces of a row
-  static constexpr int N = (C / 4) * U;                       // groups
-  static constexpr int PER = (N + NT - 1) / NT;
-  static constexpr int NTG = NT / U;                          // groups of rows the threads hold at a time
-  la_u32x4 r[PER][4];
-
-  static __device__ __forceinline__ int piece() { return threadIdx.x % U; }
-  static __device__ __forceinline__ int group() { return threadIdx.x / U; }
-
-  // rows at positions 0 .. n-1 of the block; beyond n and dim: zeros
-  __device__ __forceinline__ void load(const LinattnView& x, long long first, int back, int n, int head) {
-    const __amdgpu_buffer_rsrc_t buf = la_buffer(la_block<T>(x, first, back, head));
-    const unsigned ld = (unsigned)x.ld * (unsigned)sizeof(T);                // (at most 2^25 bytes: the host checks)
-    const int t0 = group(), t0_row = back ? C / 4 - 1 - (PER - 1) * NTG - t0 : t0;
-    const unsigned off = (unsigned)(4 * t0_row) * ld + piece() * 16;
-    const bool in_row = piece() * PIECE < x.dim;
+// E consecutive rows x 1 piece of 16 bytes; `lane` is the first row's la_lane.
+template <typename T, int E>
+__device__ __forceinline__ void la_load_group(la_u32x4 (&r)[E], const LaBlock<T>& b, unsigned lane) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const unsigned rows = back ? 4 * (PER - 1 - i) * NTG + 3 - e : 4 * i * NTG + e;
-        const bool there = in_row && 4 * (t0 + i * NTG) + e < n;
-        r[i][e] = __builtin_amdgcn_raw_buffer_load_b128(buf, there ? off : LA_NOWHERE, __builtin_amdgcn_readfirstlane(rows * ld), 0);
-      }
-  }
-};
+  for (int e = 0; e < E; ++e) r[e] = __builtin_amdgcn_raw_buffer_load_b128(b.buf, lane + b.at0 + (unsigned)(e * b.ld), 0, 0);
+}
 
 // Where an operand's rows are not made of 16-byte pieces its elements are fetched one by one when LDS is filled.
 template <typename T>
@@ -210,24 +195,448 @@ __device__ __forceinline__ T la_element(const LinattnView& x, long long first, i
   return pos < n && d < x.dim ? ((const T*)x.p)[(back ? first - pos : first + pos) * x.ld + (long long)head * x.dim + d] : (T)0;
 }
 
-template <typename T, int KT, int VT, bool OUT>
-struct LaLds;
-// bf16: q and k by rows (two quads of every 16 exchanged: the order an accumulator's rows have as an operand), k and v by
-// columns, steps in the same order, 16-byte units of a column exchanged among each other so that neither the writes by rows
-// nor the reads by columns meet in a bank
+// What a walk knows of its place.
+struct LinattnPlace {
+  LinattnSegment s;
+  int which, head, p0, p1;       // role, state head, positions in the order of the walk
+  long long first;               // row of position 0
+  long long state_at, seg_at;    // the sequence's state, the segment's place in the workspace (elements)
+  float g2;                      // log2 lambda
+};
+
+// The roles of a unit (segment, head) read the same arrays: their workgroups have numbers that are equal modulo 8, so that
+// one XCD's L2 sees all of them.
+__device__ __forceinline__ bool la_place(const LinattnArgs& a, bool out, LinattnPlace& w) {
+  const int id = blockIdx.x, pack = 8 * a.roles;
+  const int unit = id / pack * 8 + id % 8;
+  w.which = id % pack / 8;
+  if (unit >= a.slots * a.kv_heads) return false;
+  w.head = unit % a.kv_heads;
+  const int slot = unit / a.kv_heads;
+  LinattnSegment s;
+  if (!la_find(a, slot, s)) return false;
+  // (the same in every lane: they form addresses that are scalars)
+  s.b = __builtin_amdgcn_readfirstlane(s.b);
+  s.index = __builtin_amdgcn_readfirstlane(s.index);
+  s.count = __builtin_amdgcn_readfirstlane(s.count);
+  s.row0 = __builtin_amdgcn_readfirstlane(s.row0);
+  s.len = __builtin_amdgcn_readfirstlane(s.len);
+  w.s = s;
+  if (!out && s.index == s.count - 1) return false;    // (nothing follows the last segment)
+  const LinattnRole& R = a.role[w.which];
+  w.p0 = s.index * a.seg_rows;
+  w.p1 = min(w.p0 + a.seg_rows, s.len);
+  const long long row = a.offsets ? (long long)s.row0 : (long long)s.b * a.T;
+  w.first = R.back ? row + s.len - 1 : row;
+  w.state_at = ((long long)s.b * a.kv_heads + w.head) * R.dk * R.dv;
+  w.seg_at = ((long long)slot * a.kv_heads + w.head) * R.dk * R.dv;
+  w.g2 = a.log_decay[w.head] * 1.44269504088896340736f;
+  return true;
+}
+
+__device__ __forceinline__ const float* la_state_in(const LinattnRole& R, const LinattnPlace& w) {
+  return R.seg && w.s.count > 1 ? R.seg + w.seg_at : R.start ? R.start + w.state_at : nullptr;
+}
+__device__ __forceinline__ float* la_state_out(const LinattnRole& R, const LinattnPlace& w, bool out) {
+  return !out ? R.seg + w.seg_at : R.end && w.s.index == w.s.count - 1 ? R.end + w.state_at : nullptr;
+}
+
+// A value the compiler cannot know to be the one it has already.
+__device__ __forceinline__ int la_again(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+__device__ __forceinline__ la_bf16x8 la_operand(la_u32x4 x) { return __builtin_bit_cast(la_bf16x8, x); }
+// fp32 values as two bf16 parts, x = hi + lo + O(2^-18 x)
+__device__ __forceinline__ la_u32x4 la_round(la_f32x8 x) { return __builtin_bit_cast(la_u32x4, __builtin_convertvector(x, la_bf16x8)); }
+__device__ __forceinline__ la_f32x8 la_widen(la_u32x4 x) {
+  la_f32x8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[2 * i] = __uint_as_float(x[i] << 16);
+    r[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
+  }
+  return r;
+}
+__device__ __forceinline__ la_u32x4 la_rest(la_f32x8 x, la_u32x4 hi) { return la_round(x - la_widen(hi)); }
+
+// ---- bf16: blocks of 64 steps, 16 x 16 x 32 MFMA.  Two waves to 32 value columns: with 16 columns each a wave's state is 32
+// registers (keys of 128), so that 4 waves of a SIMD cover each other's waits.
+//
+// An accumulator's element e of lane l is (row 4 (l / 16) + e, column l % 16); an operand's lane holds 8 values of its row,
+// k = 8 (l / 16) ..  Two accumulators above each other are so an operand with 32 values of k in the order of quads
+// 0 4 1 5 2 6 3 7: the state and the scores become operands as they lie, and what they are multiplied with is laid out in
+// that order: q and k by rows (dims), k and v by columns (steps).
+constexpr int LA_FADE = 16;     // place of the factor lambda^0 in the table
+
 template <int KT, int VT, bool OUT>
-struct LaLds<la_bf16, KT, VT, OUT> {
-  static constexpr int PITCH = KT * 32 * 2 + 16;
+struct LaLds {
+  static constexpr int PITCH = KT * 32 * 2 + 16;                 // bytes from row to row: 16 rows in 64 banks
   __align__(16) unsigned char q[OUT ? 64 * PITCH : 16];
   __align__(16) unsigned char k[OUT ? 64 * PITCH : 16];
+  // 16-byte units of a column are exchanged (la_swizzle): neither writes by rows nor reads by columns meet in a bank
   __align__(16) unsigned char kt[KT * 32 * 128];
   __align__(16) unsigned char vt[VT * 32 * 128];
-  __align__(16) float weight[64];      // lambda^(n-1+late-j) of step j of the block: what the block's end keeps of it
-  __align__(16) float fade[96];        // p_scale lambda^m at 31 + m, zeros before: the factor of a pair of steps m apart
-  __align__(16) unsigned char p[OUT ? 3 : 1][2][2][64 * 16];   // scores as operands: tile, half of its steps, part, lane
+  __align__(16) unsigned char p[OUT ? 6 : 1][2][64 * 16];        // scores as operands: pair of tiles, part, lane
+  __align__(16) float fade[OUT ? LA_FADE + 64 : 4];              // p_scale lambda^m at LA_FADE + m, zeros before
+  __align__(16) float weight[64];                                // lambda^(n-1+late-j): what the block's end keeps of step j
 };
+
+__device__ __forceinline__ int la_swizzle(int d) { return ((d >> 1) ^ (d >> 4)) & 7; }
+__device__ __forceinline__ int la_quad(int q) { return (q & 3) * 2 + (q >> 2 & 1); }       // place of quad q of 8
+
+__device__ __forceinline__ uint32_t la_pack(float x, float y) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 pair;
+  const pair h = {(__bf16)x, (__bf16)y};
+  return __builtin_bit_cast(uint32_t, h);
+}
+
+// place of the scores of queries 16 it .. and steps 32 kb .. (the second halves of 0 and 3 lie above the diagonal)
+__device__ __forceinline__ constexpr int la_pair(int it, int kb) { return it < 2 ? it : 2 * it - 2 + kb; }
+
+// rows p .. p + rows - 1, piece u
+__device__ __forceinline__ void la_put_rows(const la_u32x4* r, int rows, unsigned char* dst, int pitch, int p, int u) {
+  unsigned char* at = dst + p * pitch + (u >> 2) * 64 + la_quad(2 * u & 7) * 8;            // (quad 2 u + 1 lies two places on)
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (e < rows) {
+      *(la_u32x2*)(at + e * pitch) = la_u32x2{r[e][0], r[e][1]};
+      *(la_u32x2*)(at + e * pitch + 16) = la_u32x2{r[e][2], r[e][3]};
+    }
+  }
+}
+
+// rows 4 tg .. 4 tg + 3, piece u, turned over
+__device__ __forceinline__ void la_put_columns(const la_u32x4 (&r)[4], unsigned char* dst, int tg, int u) {
+  // (la_swizzle(8 u + dd) = la_swizzle(8 u) ^ dd / 2: four addresses and fixed distances from them)
+  unsigned char* column = dst + 8 * u * 128 + (tg >> 2 & 1) * 8;
+  const int unit = (4 * (tg >> 3) + (tg & 3)) ^ la_swizzle(8 * u);
+#pragma unroll
+  for (int dd = 0; dd < 8; ++dd) {
+    const uint32_t sel = dd & 1 ? 0x07060302u : 0x05040100u;
+    la_u32x2 o;
+    o[0] = __builtin_amdgcn_perm(r[1][dd / 2], r[0][dd / 2], sel);
+    o[1] = __builtin_amdgcn_perm(r[3][dd / 2], r[2][dd / 2], sel);
+    *(la_u32x2*)(column + ((unit ^ (dd / 2)) * 16) + dd * 128) = o;
+  }
+}
+
+template <int TILES, int NT>
+__device__ __forceinline__ void la_fetch_rows(const LinattnView& x, long long first, int back, int n, int head, unsigned char* dst, int pitch) {
+#pragma unroll 4
+  for (int i = threadIdx.x; i < 64 * 32 * TILES; i += NT) {
+    const int pos = i / (32 * TILES), d = i % (32 * TILES);
+    *(la_bf16*)(dst + pos * pitch + (d >> 5) * 64 + la_quad(d >> 2 & 7) * 8 + (d & 3) * 2) = la_element<la_bf16>(x, first, back, n, head, pos, d);
+  }
+}
+
+template <int TILES, int NT>
+__device__ __forceinline__ void la_fetch_columns(const LinattnView& x, long long first, int back, int n, int head, unsigned char* dst) {
+#pragma unroll 4
+  for (int i = threadIdx.x; i < 64 * 32 * TILES; i += NT) {
+    const int pos = i / (32 * TILES), d = i % (32 * TILES), tg = pos >> 2;
+    *(la_bf16*)(dst + d * 128 + ((4 * (tg >> 3) + (tg & 3)) ^ la_swizzle(d)) * 16 + (tg >> 2 & 1) * 8 + (pos & 3) * 2) =
+        la_element<la_bf16>(x, first, back, n, head, pos, d);
+  }
+}
+
+__device__ __forceinline__ la_f32x4 la_mfma16(la_u32x4 x, la_u32x4 y, la_f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(la_operand(x), la_operand(y), c, 0, 0, 0);
+}
+
+// OUT = true: the walk with outputs.  OUT = false: only the state a segment adds, from zero, into the workspace.
+// VEC: every operand's rows come in 16-byte pieces (else none is taken to).
+template <int KT, int VT, bool OUT, bool VEC>
+__global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_kernel(LinattnArgs a) {
+  constexpr int C = LA_BF16_ROWS, NT = 128 * VT, NW = 2 * VT;
+  __shared__ LaLds<KT, VT, OUT> lds;
+  LinattnPlace w;
+  if (!la_place(a, OUT, w)) return;
+  const LinattnRole& R = a.role[w.which];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int cl = lane & 15, g = lane >> 4;
+  const int late = R.back, head = w.head, gq = R.gq, gk = R.gk;
+  const int dk = R.dk, dv = R.dv, st_r = R.st_r, parts = R.parts;
+  const float g2 = w.g2;
+
+  // ---- state: element e of tile t is (key 16 t + 4 g + e, value 16 wave + cl)
+  la_f32x4 S[2 * KT];
+  const int col = 16 * wave + cl;
+  unsigned state_off = (unsigned)(4 * g * R.st_r + col * R.st_c) * 4;
+  if (OUT) {
+    const float* src = la_state_in(R, w);
+    const __amdgpu_buffer_rsrc_t buf = la_buffer(src);
+#pragma unroll
+    for (int t = 0; t < 2 * KT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = 16 * t + e;
+        const bool there = (src != nullptr) & (key + 4 * g < dk) & (col < dv);
+        S[t][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buf, there ? state_off : LA_NOWHERE, key * st_r * 4, 0));
+      }
+  } else {
+#pragma unroll
+    for (int t = 0; t < 2 * KT; ++t) S[t] = la_f32x4{};
+  }
+
+  if (OUT) {
+    for (int i = threadIdx.x; i < LA_FADE + 64; i += NT) lds.fade[i] = i < LA_FADE ? 0.0f : R.p_scale * la_pow(g2, i - LA_FADE);
+    // (tiles above the diagonal: the second halves of pairs 0 and 3)
+    for (int i = threadIdx.x; i < 4 * 64; i += NT) *(la_u32x2*)&lds.p[(i >> 7) * 3][i >> 6 & 1][(i & 63) * 16 + 8] = la_u32x2{};
+  }
+
+  const int stages = gq > gk ? gq : gk;
+  const auto q_head = [&](int st) { return head * gq + (gq > 1 ? st : 0); };
+  const auto k_head = [&](int st) { return head * gk + (gk > 1 ? st : 0); };
+  // The next block's pieces, always into the same registers: what a stage does not need is asked for from nowhere (a branch
+  // around the loads would have their results moved, and so waited for, where it ends).  Groups of 4 rows of k, then of v:
+  // 64 to a wave, so that a wave's are all of one array.
+  constexpr int PER = (KT + VT + NW - 1) / NW, PERQ = (KT + VT - 1) / VT;
+  la_u32x4 kv[PER][4], qs[PERQ][2];
+  unsigned kv_lane[PER], q_lane[PERQ];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int part = wave + i * NW;                                          // of KT + VT parts of 64 groups
+    const bool keys = part < KT;
+    const int at = (keys ? part : part - KT) * 64 + lane, U = keys ? 4 * KT : 4 * VT;
+    const LinattnView x = keys ? R.k : R.v;
+    kv_lane[i] = part < KT + VT ? la_lane<la_bf16>(x, R.back, at / U * 4, at % U * 8) : LA_NOWHERE;
+  }
+#pragma unroll
+  for (int i = 0; i < PERQ; ++i) {
+    const int at = threadIdx.x + i * NT;
+    q_lane[i] = at < 128 * KT ? la_lane<la_bf16>(R.q, R.back, at / (4 * KT) * 2, at % (4 * KT) * 8) : LA_NOWHERE;
+  }
+  auto request = [&](int p, int st) {
+    const long long row = R.back ? w.first - p : w.first + p;
+    const int n = max(0, min(C, w.p1 - p));                                  // (none behind the last block)
+    const int nk = gk > 1 || st == 0 ? n : 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const LinattnView x = wave + i * NW < KT ? R.k : R.v;
+      la_load_group(kv[i], la_block<la_bf16>(x, row, R.back, nk, k_head(st)), kv_lane[i]);
+    }
+    if (OUT) {
+      const LaBlock<la_bf16> q = la_block<la_bf16>(R.q, row, R.back, gq > 1 || st == 0 ? n : 0, q_head(st));
+#pragma unroll
+      for (int i = 0; i < PERQ; ++i) la_load_group(qs[i], q, q_lane[i]);
+    }
+  };
+  if (VEC) request(w.p0, 0);
+
+  // The state in the registers is the state divided by `frame`: a block's decay goes into `frame` and only where that leaves
+  // 2^-30 .. 2^30 into the 2 KT x 4 registers.
+  float frame = 1.0f;
+
+  la_f32x4 O[4];
+  for (int p = w.p0; p < w.p1; p += C) {
+    const int n = min(C, w.p1 - p);
+    float next = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(frame * la_pow(g2, n))));
+    const bool rescale = !(next >= 0x1p-30f && next <= 0x1p30f);
+    const float factor = next;
+    next = rescale ? 1.0f : next;
+    const long long row = R.back ? w.first - p : w.first + p;
+    for (int st = 0; st < stages; ++st) {
+      const bool new_q = gq > 1 || st == 0, new_kv = gk > 1 || st == 0, last = st == stages - 1;
+      __syncthreads();                       // every wave has read the block before
+      if (VEC) {
+        const int lane = la_again(threadIdx.x & 63);
+        if (OUT && new_q) {
+#pragma unroll
+          for (int i = 0; i < PERQ; ++i) {
+            const int at = 64 * wave + lane + i * NT;
+            if (at < 128 * KT) la_put_rows(qs[i], 2, lds.q, lds.PITCH, at / (4 * KT) * 2, at % (4 * KT));
+          }
+        }
+        if (new_kv) {
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            const int part = wave + i * NW;
+            if (part < KT) {
+              const int at = part * 64 + lane, tg = at / (4 * KT), u = at % (4 * KT);
+              if (OUT) la_put_rows(kv[i], 4, lds.k, lds.PITCH, 4 * tg, u);
+              la_put_columns(kv[i], lds.kt, tg, u);
+            } else if (part < KT + VT) {
+              const int at = (part - KT) * 64 + lane;
+              la_put_columns(kv[i], lds.vt, at / (4 * VT), at % (4 * VT));
+            }
+          }
+        }
+      } else {
+        if (OUT && new_q) la_fetch_rows<KT, NT>(R.q, row, R.back, n, q_head(st), lds.q, lds.PITCH);
+        if (new_kv) {
+          if (OUT) la_fetch_rows<KT, NT>(R.k, row, R.back, n, k_head(st), lds.k, lds.PITCH);
+          la_fetch_columns<KT, NT>(R.k, row, R.back, n, k_head(st), lds.kt);
+          la_fetch_columns<VT, NT>(R.v, row, R.back, n, k_head(st), lds.vt);
+        }
+      }
+      if (new_kv && wave == 0) {
+        const int j = la_again(threadIdx.x & 63);
+        lds.weight[j] = R.s_scale / next * la_pow(g2, max(0, n - 1 + late - j));
+      }
+      if (VEC) request(last ? p + C : p, last ? 0 : st + 1);
+      __syncthreads();
+
+      // (what a lane's number makes of addresses is formed again for every product: kept, it would take the registers that
+      // let four waves share a SIMD)
+      if (OUT) {
+        {
+        const int lane = la_again(threadIdx.x & 63), cl = lane & 15, g = lane >> 4;
+        const unsigned char* q_ = lds.q + cl * lds.PITCH + g * 16;
+        const unsigned char* k_ = lds.k + cl * lds.PITCH + g * 16;
+        // Scores of the 10 tiles (steps jt <= queries it), transposed, divided among the waves: every wave needs them all, as
+        // operands in two parts, and gets them through LDS while its product with the state runs.
+        for (int t = wave; t < 10; t += NW) {
+          const int it = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, jt = t - it * (it + 1) / 2;
+          const unsigned char* qt = q_ + it * 16 * lds.PITCH;
+          const unsigned char* kr = k_ + jt * 16 * lds.PITCH;
+          la_f32x4 P = {};
+          la_u32x4 qf[KT], kf[KT];
+#pragma unroll
+          for (int kb = 0; kb < KT; ++kb) {
+            qf[kb] = *(const la_u32x4*)(qt + kb * 64);
+            kf[kb] = *(const la_u32x4*)(kr + kb * 64);
+          }
+          __builtin_amdgcn_sched_barrier(0);      // (all requested before the first is waited for)
+#pragma unroll
+          for (int kb = 0; kb < KT; ++kb) P = la_mfma16(kf[kb], qf[kb], P);
+          const float* f = lds.fade + LA_FADE + 16 * (it - jt) + cl - 4 * g;
+          uint32_t hi[2], lo[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float x = P[2 * e] * f[-2 * e], y = P[2 * e + 1] * f[-2 * e - 1];
+            hi[e] = la_pack(x, y);
+            lo[e] = la_pack(x - __uint_as_float(hi[e] << 16), y - __uint_as_float(hi[e] & 0xffff0000u));
+          }
+          *(la_u32x2*)&lds.p[la_pair(it, jt >> 1)][0][lane * 16 + (jt & 1) * 8] = la_u32x2{hi[0], hi[1]};
+          *(la_u32x2*)&lds.p[la_pair(it, jt >> 1)][1][lane * 16 + (jt & 1) * 8] = la_u32x2{lo[0], lo[1]};
+        }
+        }
+        if (new_q) {
+          const int lane = la_again(threadIdx.x & 63);
+          const unsigned char* q_ = lds.q + (lane & 15) * lds.PITCH + (lane >> 4) * 16;
+          auto q_frag = [&](int it, int kb) { return *(const la_u32x4*)(q_ + it * 16 * lds.PITCH + kb * 64); };
+          // O^T = S^T Q^T: the accumulator of the state is an operand as it lies
+          la_u32x4 qf[2][4];
+#pragma unroll
+          for (int it = 0; it < 4; ++it) qf[0][it] = q_frag(it, 0);
+#pragma unroll
+          for (int kb = 0; kb < KT; ++kb) {
+            // (the next operands are on their way while these are multiplied; equal accumulators lie four MFMAs apart)
+            if (kb + 1 < KT) {
+#pragma unroll
+              for (int it = 0; it < 4; ++it) qf[(kb + 1) & 1][it] = q_frag(it, kb + 1);
+            }
+            const la_f32x8 x = __builtin_shufflevector(S[2 * kb], S[2 * kb + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+            const la_u32x4 hi = la_round(x), lo = la_rest(x, hi);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int it = 0; it < 4; ++it) O[it] = la_mfma16(hi, qf[kb & 1][it], kb == 0 ? la_f32x4{} : O[it]);
+#pragma unroll
+            for (int it = 0; it < 4; ++it) O[it] = la_mfma16(lo, qf[kb & 1][it], O[it]);
+          }
+          float f = R.i_scale * frame * la_pow(g2, (lane & 15) + 1 - late);
+          const float to16 = la_pow(g2, 16);
+#pragma unroll
+          for (int it = 0; it < 4; ++it) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) O[it][e] *= f;
+            f *= to16;
+          }
+        }
+        __syncthreads();
+      }
+      const int lane = la_again(threadIdx.x & 63), cl = lane & 15, g = lane >> 4;
+      // (la_swizzle(16 t + c) = la_swizzle(c) ^ t for c < 16)
+      const unsigned char* kt_ = lds.kt + cl * 128;
+      const unsigned char* vt_ = lds.vt + (16 * wave + cl) * 128;
+      const int ksw = (g ^ la_swizzle(cl)) * 16, vsw = (g ^ la_swizzle(16 * wave + cl)) * 16;
+      auto v_frag = [&](int kb) { return *(const la_u32x4*)(vt_ + (vsw ^ 64 * kb)); };
+      auto kt_frag = [&](int t, int kb) { return *(const la_u32x4*)(kt_ + (ksw ^ 16 * (4 * kb ^ (t & 7))) + t * 16 * 128); };
+      if (OUT) {
+        // O^T += V^T P^T
+        la_u32x4 pf[2][6], vf[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) vf[kb] = v_frag(kb);
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+#pragma unroll
+          for (int i = 0; i < 6; ++i) pf[part][i] = *(const la_u32x4*)&lds.p[i][part][lane * 16];
+          if (part == 0) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int it = 0; it < 4; ++it) O[it] = la_mfma16(vf[0], pf[part][la_pair(it, 0)], O[it]);
+#pragma unroll
+          for (int it = 2; it < 4; ++it) O[it] = la_mfma16(vf[1], pf[part][la_pair(it, 1)], O[it]);
+        }
+      }
+      if (OUT && (gq > 1 || last)) {
+        // element e of tile it is (value 16 wave + 4 g + e, step 16 it + cl)
+        const LaBlock<la_bf16> o = la_block<la_bf16>(R.o, row, R.back, n, q_head(st));
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          const unsigned at = la_lane<la_bf16>(R.o, R.back, cl, 16 * wave + 4 * g) + o.at0 + (unsigned)(16 * it * o.ld);
+          const la_u32x2 y = {la_pack(O[it][0], O[it][1]), la_pack(O[it][2], O[it][3])};
+          if (VEC) {
+            __builtin_amdgcn_raw_buffer_store_b64(y, o.buf, at, 0, 0);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              __builtin_amdgcn_raw_buffer_store_b16((short)(y[i / 2] >> 16 * (i & 1)), o.buf, 16 * wave + 4 * g + i < dv ? at + 2 * i : LA_NOWHERE, 0, 0);
+          }
+        }
+      }
+      // S = lambda^n S + K^T V'
+      if (rescale && (gk > 1 ? st == 0 : last)) {
+#pragma unroll
+        for (int t = 0; t < 2 * KT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) S[t][e] *= factor;
+      }
+      if (gk > 1 || last) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const la_f32x4 w0 = *(const la_f32x4*)&lds.weight[32 * kb + 4 * g], w1 = *(const la_f32x4*)&lds.weight[32 * kb + 16 + 4 * g];
+          const la_f32x8 x = la_widen(v_frag(kb)) * __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7);
+          const la_u32x4 h0 = la_round(x), h1 = la_rest(x, h0);
+#pragma unroll
+          for (int t = 0; t < 2 * KT; ++t) {
+            const la_u32x4 kf = kt_frag(t, kb);
+            S[t] = la_mfma16(kf, h0, S[t]);
+            S[t] = la_mfma16(kf, h1, S[t]);
+          }
+          if (parts > 2) {
+            asm volatile("" ::: "memory");      // (k is read again, not kept)
+            const la_u32x4 h2 = la_rest(x - la_widen(h0), h1);
+#pragma unroll
+            for (int t = 0; t < 2 * KT; ++t) S[t] = la_mfma16(kt_frag(t, kb), h2, S[t]);
+          }
+        }
+      }
+    }
+    frame = next;
+  }
+
+  float* dst = la_state_out(R, w, OUT);
+  if (dst) {
+    const __amdgpu_buffer_rsrc_t buf = la_buffer(dst);
+    int key0 = 4 * g, col0 = col;
+    asm volatile("" : "+v"(state_off), "+v"(key0), "+v"(col0));      // (formed again, not kept from the loads)
+#pragma unroll
+    for (int t = 0; t < 2 * KT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = 16 * t + e;
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[t][e] * frame), buf, ((key + key0 < dk) & (col0 < dv)) ? state_off : LA_NOWHERE,
+                                              key * st_r * 4, 0);
+      }
+  }
+}
+
+// ---- fp32: blocks of 32 steps, 32 x 32 x 2 MFMA (an accumulator's rows are operand values as they lie, so nothing is turned
+// over).  Wave w holds the value columns 32 w .. 32 w + 31.
 template <int KT, int VT, bool OUT>
-struct LaLds<float, KT, VT, OUT> {
+struct LaLdsF32 {
   static constexpr int PITCH = KT * 32 + 4, VPITCH = VT * 32 + 4;
   __align__(16) float q[OUT ? 32 * PITCH : 4];
   __align__(16) float k[32 * PITCH];
@@ -236,89 +645,6 @@ struct LaLds<float, KT, VT, OUT> {
   __align__(16) float fade[64];
   la_f32x4 p[OUT ? VT : 1][4][64];     // each wave's share of the scores' sums: quad of rows, lane
 };
-
-__device__ __forceinline__ int la_swizzle(int d) { return ((d >> 1) ^ (d >> 4)) & 7; }
-
-// place of step `pos` (of the block) in a column, in bf16 elements: unit of 8, quad and element of the quad
-__device__ __forceinline__ int la_unit(int tg) { return 2 * (tg >> 2) + (tg & 1); }       // tg = pos / 4
-__device__ __forceinline__ int la_half(int tg) { return (tg >> 1) & 1; }
-
-template <int TILES, int NT>
-__device__ __forceinline__ void la_put_rows(const LaStage<la_bf16, TILES, NT>& st, unsigned char* dst, int pitch) {
-  typedef LaStage<la_bf16, TILES, NT> S;
-  const int u = S::piece(), t0 = S::group();
-#pragma unroll
-  for (int i = 0; i < S::PER; ++i) {
-    const int tg = t0 + i * S::NTG;
-    if (tg < 16) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        unsigned char* p = dst + (4 * tg + e) * pitch + (u >> 1) * 32 + (u & 1) * 8;
-        *(uint2*)p = make_uint2(st.r[i][e][0], st.r[i][e][1]);
-        *(uint2*)(p + 16) = make_uint2(st.r[i][e][2], st.r[i][e][3]);
-      }
-    }
-  }
-}
-
-template <int TILES, int NT>
-__device__ __forceinline__ void la_put_columns(const LaStage<la_bf16, TILES, NT>& st, unsigned char* dst) {
-  typedef LaStage<la_bf16, TILES, NT> S;
-  const int u = S::piece(), t0 = S::group();
-#pragma unroll
-  for (int i = 0; i < S::PER; ++i) {
-    const int tg = t0 + i * S::NTG;
-    if (tg < 16) {
-      // (la_swizzle(8 u + dd) = la_swizzle(8 u) ^ dd / 2: four addresses and fixed distances from them)
-      unsigned char* column = dst + 8 * u * 128 + la_half(tg) * 8;
-      const int unit = la_unit(tg) ^ la_swizzle(8 * u);
-#pragma unroll
-      for (int dd = 0; dd < 8; ++dd) {
-        const uint32_t sel = dd & 1 ? 0x07060302u : 0x05040100u;
-        uint2 o;
-        o.x = __builtin_amdgcn_perm(st.r[i][1][dd / 2], st.r[i][0][dd / 2], sel);
-        o.y = __builtin_amdgcn_perm(st.r[i][3][dd / 2], st.r[i][2][dd / 2], sel);
-        *(uint2*)(column + ((unit ^ (dd / 2)) * 16) + dd * 128) = o;
-      }
-    }
-  }
-}
-
-template <int TILES, int NT>
-__device__ __forceinline__ void la_put_rows(const LaStage<float, TILES, NT>& st, float* dst, int pitch) {
-  typedef LaStage<float, TILES, NT> S;
-  const int u = S::piece(), t0 = S::group();
-#pragma unroll
-  for (int i = 0; i < S::PER; ++i) {
-    const int tg = t0 + i * S::NTG;
-    if (tg < 8) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) *(la_u32x4*)(dst + (4 * tg + e) * pitch + 4 * u) = st.r[i][e];
-    }
-  }
-}
-
-// the same from memory, element by element
-template <int TILES, int NT>
-__device__ __forceinline__ void la_fetch_rows(const LinattnView& x, long long first, int back, int n, int head, unsigned char* dst, int pitch) {
-#pragma unroll 4
-  for (int i = threadIdx.x; i < 64 * 32 * TILES; i += NT) {
-    const int pos = i / (32 * TILES), d = i % (32 * TILES);
-    // quads 1 and 2 of every 16 elements are exchanged
-    const int at = (d & ~12) | (d & 4) << 1 | (d & 8) >> 1;
-    *(la_bf16*)(dst + pos * pitch + 2 * at) = la_element<la_bf16>(x, first, back, n, head, pos, d);
-  }
-}
-
-template <int TILES, int NT>
-__device__ __forceinline__ void la_fetch_columns(const LinattnView& x, long long first, int back, int n, int head, unsigned char* dst) {
-#pragma unroll 4
-  for (int i = threadIdx.x; i < 64 * 32 * TILES; i += NT) {
-    const int pos = i / (32 * TILES), d = i % (32 * TILES), tg = pos / 4;
-    *(la_bf16*)(dst + d * 128 + (la_unit(tg) ^ la_swizzle(d)) * 16 + la_half(tg) * 8 + (pos & 3) * 2) =
-        la_element<la_bf16>(x, first, back, n, head, pos, d);
-  }
-}
 
 template <int TILES, int NT>
 __device__ __forceinline__ void la_fetch_rows(const LinattnView& x, long long first, int back, int n, int head, float* dst, int pitch) {
@@ -329,312 +655,194 @@ __device__ __forceinline__ void la_fetch_rows(const LinattnView& x, long long fi
   }
 }
 
-// fp32 values as two bf16 parts, x = hi + lo + O(2^-17 x)
-__device__ __forceinline__ la_bf16x8 la_round(la_f32x8 x) { return __builtin_convertvector(x, la_bf16x8); }
-__device__ __forceinline__ la_bf16x8 la_rest(la_f32x8 x, la_bf16x8 hi) { return la_round(x - __builtin_convertvector(hi, la_f32x8)); }
+// groups of 4 rows x 16 bytes
+template <int TILES, int PER, int NT>
+__device__ __forceinline__ void la_put_rows(const la_u32x4 (&r)[PER][4], float* dst, int pitch) {
+  constexpr int U = TILES * 8;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int at = threadIdx.x + i * NT;
+    if (at < 8 * U) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *(la_u32x4*)(dst + (at / U * 4 + e) * pitch + 4 * (at % U)) = r[i][e];
+    }
+  }
+}
 
-// OUT = true: the walk with outputs.  OUT = false: only the state a segment adds, from zero, into the workspace.
-// VEC: every operand's rows come in 16-byte pieces (else none is taken to).
-template <typename T, int KT, int VT, bool OUT, bool VEC>
-__global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(LinattnArgs a) {
-  constexpr bool F32 = sizeof(T) == 4;
-  constexpr int C = LaShape<T>::C, IT = C / 32, NT = 64 * VT;
-  __shared__ LaLds<T, KT, VT, OUT> lds;
-
-  // the roles of a unit (segment, head) read the same arrays: their workgroups have numbers that are equal modulo 8, so
-  // that one XCD's L2 sees all of them
-  const int id = blockIdx.x, pack = 8 * a.roles;
-  const int unit = id / pack * 8 + id % 8, which = id % pack / 8;
-  if (unit >= a.slots * a.kv_heads) return;
-  const LinattnRole& R = a.role[which];
-  const int head = unit % a.kv_heads;
-  LinattnSegment s;
-  if (!la_find(a, unit / a.kv_heads, s)) return;
-  // (the same in every lane: they form addresses that are scalars)
-  s.b = __builtin_amdgcn_readfirstlane(s.b);
-  s.index = __builtin_amdgcn_readfirstlane(s.index);
-  s.count = __builtin_amdgcn_readfirstlane(s.count);
-  s.row0 = __builtin_amdgcn_readfirstlane(s.row0);
-  s.len = __builtin_amdgcn_readfirstlane(s.len);
-  if (!OUT && s.index == s.count - 1) return;    // (nothing follows the last segment)
-
+template <int KT, int VT, bool OUT, bool VEC>
+__global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_f32_kernel(LinattnArgs a) {
+  constexpr int C = LA_F32_ROWS, NT = 64 * VT;
+  __shared__ LaLdsF32<KT, VT, OUT> lds;
+  LinattnPlace w;
+  if (!la_place(a, OUT, w)) return;
+  const LinattnRole& R = a.role[w.which];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int cl = lane & 31, hh = lane >> 5;
-  const float g2 = a.log_decay[head] * 1.44269504088896340736f;
-  const int late = R.back;
-  const int p0 = s.index * a.seg_rows, p1 = min(p0 + a.seg_rows, s.len);    // positions in the order of the walk
-  const long long seq_row = a.offsets ? (long long)s.row0 : (long long)s.b * a.T;
-  const long long first = R.back ? seq_row + s.len - 1 : seq_row;           // row of position 0
-  const long long state_at = ((long long)s.b * a.kv_heads + head) * R.dk * R.dv;
+  const int late = R.back, head = w.head, gq = R.gq, gk = R.gk;
+  const int dk = R.dk, dv = R.dv, st_r = R.st_r;
+  const float g2 = w.g2;
 
   // ---- state: element e = 4 jj + i of tile kt is (key 32 kt + 8 jj + 4 hh + i, value 32 wave + cl)
   la_f32x16 S[KT];
   const int col = 32 * wave + cl;
   unsigned state_off = (unsigned)(4 * hh * R.st_r + col * R.st_c) * 4;
-  const long long seg_at = ((long long)(unit / a.kv_heads) * a.kv_heads + head) * R.dk * R.dv;
-  {
-    const float* src = !OUT ? nullptr : R.seg && s.count > 1 ? R.seg + seg_at : R.start ? R.start + state_at : nullptr;
+  if (OUT) {
+    const float* src = la_state_in(R, w);
     const __amdgpu_buffer_rsrc_t buf = la_buffer(src);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int key = 32 * kt + 8 * (e / 4) + e % 4;
-        const bool there = src && key + 4 * hh < R.dk && col < R.dv;
-        S[kt][e] = OUT ? __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buf, there ? state_off : LA_NOWHERE, key * R.st_r * 4, 0)) : 0.0f;
+        const bool there = (src != nullptr) & (key + 4 * hh < dk) & (col < dv);
+        S[kt][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buf, there ? state_off : LA_NOWHERE, key * st_r * 4, 0));
       }
-  }
-
-  float row_in[IT];
-  if (OUT) {
-    for (int i = threadIdx.x; i < C + 32; i += NT) lds.fade[i] = i < 31 ? 0.0f : R.p_scale * la_pow(g2, i - 31);
+  } else {
 #pragma unroll
-    for (int it = 0; it < IT; ++it) row_in[it] = R.i_scale * la_pow(g2, 32 * it + cl + 1 - late);
+    for (int kt = 0; kt < KT; ++kt) S[kt] = la_f32x16{};
   }
 
-  LaStage<T, KT, NT> qs, ks;
-  LaStage<T, VT, NT> vs;
-  const int stages = R.gq > R.gk ? R.gq : R.gk;
-  const auto q_head = [&](int st) { return head * R.gq + (R.gq > 1 ? st : 0); };
-  const auto k_head = [&](int st) { return head * R.gk + (R.gk > 1 ? st : 0); };
-  // The next block's pieces, always into the same registers: what a stage does not need is asked for from nowhere (a branch
-  // around the loads would have their results moved, and so waited for, where it ends).
-  auto request = [&](int p, int st) {
-    const long long row = R.back ? first - p : first + p;
-    const int n = min(C, p1 - p);                                          // (none behind the last block)
-    if (OUT && VEC) qs.load(R.q, row, R.back, R.gq > 1 || st == 0 ? n : 0, q_head(st));
-    if (VEC) {
-      const int nk = R.gk > 1 || st == 0 ? n : 0;
-      ks.load(R.k, row, R.back, nk, k_head(st));
-      vs.load(R.v, row, R.back, nk, k_head(st));
-    }
-  };
-  request(p0, 0);
+  float row_in = 0.0f;
+  if (OUT) {
+    for (int i = threadIdx.x; i < 64; i += NT) lds.fade[i] = i < 31 ? 0.0f : R.p_scale * la_pow(g2, i - 31);
+    row_in = R.i_scale * la_pow(g2, cl + 1 - late);
+  }
 
-  la_f32x16 O[IT];
-  for (int p = p0; p < p1; p += C) {
-    const int n = min(C, p1 - p);
+  const int stages = gq > gk ? gq : gk;
+  const auto q_head = [&](int st) { return head * gq + (gq > 1 ? st : 0); };
+  const auto k_head = [&](int st) { return head * gk + (gk > 1 ? st : 0); };
+  constexpr int PERK = (KT + VT - 1) / VT;
+  la_u32x4 qs[PERK][4], ks[PERK][4], vs[1][4];
+  unsigned q_lane[PERK], k_lane[PERK];
+#pragma unroll
+  for (int i = 0; i < PERK; ++i) {
+    const int at = threadIdx.x + i * NT, p4 = at / (8 * KT) * 4, d = at % (8 * KT) * 4;
+    q_lane[i] = OUT && at < 64 * KT ? la_lane<float>(R.q, R.back, p4, d) : LA_NOWHERE;
+    k_lane[i] = at < 64 * KT ? la_lane<float>(R.k, R.back, p4, d) : LA_NOWHERE;
+  }
+  const unsigned v_lane = la_lane<float>(R.v, R.back, (int)threadIdx.x / (8 * VT) * 4, (int)threadIdx.x % (8 * VT) * 4);
+  auto request = [&](int p, int st) {           // (as in the bf16 walk: always into the same registers)
+    const long long row = R.back ? w.first - p : w.first + p;
+    const int n = max(0, min(C, w.p1 - p)), nk = gk > 1 || st == 0 ? n : 0;
+    const LaBlock<float> k = la_block<float>(R.k, row, R.back, nk, k_head(st));
+    if (OUT) {
+      const LaBlock<float> q = la_block<float>(R.q, row, R.back, gq > 1 || st == 0 ? n : 0, q_head(st));
+#pragma unroll
+      for (int i = 0; i < PERK; ++i) la_load_group(qs[i], q, q_lane[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < PERK; ++i) la_load_group(ks[i], k, k_lane[i]);
+    la_load_group(vs[0], la_block<float>(R.v, row, R.back, nk, k_head(st)), v_lane);
+  };
+  if (VEC) request(w.p0, 0);
+
+  la_f32x16 O;
+  for (int p = w.p0; p < w.p1; p += C) {
+    const int n = min(C, w.p1 - p);
     const float keep = la_pow(g2, n);
+    const long long row = R.back ? w.first - p : w.first + p;
     for (int st = 0; st < stages; ++st) {
-      const bool new_q = R.gq > 1 || st == 0, new_kv = R.gk > 1 || st == 0, last = st == stages - 1;
+      const bool new_q = gq > 1 || st == 0, new_kv = gk > 1 || st == 0, last = st == stages - 1;
       __syncthreads();                       // every wave has read the block before
-      const long long row = R.back ? first - p : first + p;
       if (OUT && new_q) {
-        if (VEC) la_put_rows(qs, lds.q, lds.PITCH);
+        if (VEC) la_put_rows<KT, PERK, NT>(qs, lds.q, lds.PITCH);
         else la_fetch_rows<KT, NT>(R.q, row, R.back, n, q_head(st), lds.q, lds.PITCH);
       }
       if (new_kv) {
-        if constexpr (F32) {
-          if (VEC) la_put_rows(ks, lds.k, lds.PITCH);
-          else la_fetch_rows<KT, NT>(R.k, row, R.back, n, k_head(st), lds.k, lds.PITCH);
-          if (VEC) la_put_rows(vs, lds.v, lds.VPITCH);
-          else la_fetch_rows<VT, NT>(R.v, row, R.back, n, k_head(st), lds.v, lds.VPITCH);
+        if (VEC) {
+          la_put_rows<KT, PERK, NT>(ks, lds.k, lds.PITCH);
+          la_put_rows<VT, 1, NT>(vs, lds.v, lds.VPITCH);
         } else {
-          if (VEC) {
-            if (OUT) la_put_rows(ks, lds.k, lds.PITCH);
-            la_put_columns(ks, lds.kt);
-          } else {
-            if (OUT) la_fetch_rows<KT, NT>(R.k, row, R.back, n, k_head(st), lds.k, lds.PITCH);
-            la_fetch_columns<KT, NT>(R.k, row, R.back, n, k_head(st), lds.kt);
-          }
-          if (VEC) la_put_columns(vs, lds.vt);
-          else la_fetch_columns<VT, NT>(R.v, row, R.back, n, k_head(st), lds.vt);
+          la_fetch_rows<KT, NT>(R.k, row, R.back, n, k_head(st), lds.k, lds.PITCH);
+          la_fetch_rows<VT, NT>(R.v, row, R.back, n, k_head(st), lds.v, lds.VPITCH);
         }
         if (threadIdx.x < C) lds.weight[threadIdx.x] = R.s_scale * la_pow(g2, max(0, n - 1 + late - (int)threadIdx.x));
       }
-      request(last ? p + C : p, last ? 0 : st + 1);
+      if (VEC) request(last ? p + C : p, last ? 0 : st + 1);
       __syncthreads();
 
-      if constexpr (!F32) {
-        // (la_swizzle(32 n + c) = la_swizzle(c) ^ 2 n: unit 2 mb + hh of column 32 kt + cl lies where mb ^ kt says)
-        const unsigned char* kt_ = lds.kt + cl * 128;
-        const unsigned char* vt_ = lds.vt + (32 * wave + cl) * 128;
-        const int ksw = (hh ^ la_swizzle(cl)) * 16, vsw = (hh ^ la_swizzle(32 * wave + cl)) * 16;
-        auto v_frag = [&](int mb) { return __builtin_bit_cast(la_bf16x8, *(const uint4*)(vt_ + (vsw ^ 32 * mb))); };
-        auto kt_frag = [&](int kt, int mb) {
-          return __builtin_bit_cast(la_bf16x8, *(const uint4*)(kt_ + (ksw ^ 32 * (mb ^ kt)) + kt * 32 * 128));
-        };
-        if (OUT) {
-          const unsigned char* q_ = lds.q + cl * lds.PITCH + hh * 16;
-          const unsigned char* k_ = lds.k + cl * lds.PITCH + hh * 16;
-          auto q_frag = [&](int it, int m) { return __builtin_bit_cast(la_bf16x8, *(const uint4*)(q_ + it * 32 * lds.PITCH + m * 32)); };
-          auto k_frag = [&](int jt, int m) { return __builtin_bit_cast(la_bf16x8, *(const uint4*)(k_ + jt * 32 * lds.PITCH + m * 32)); };
-          // Scores of the tiles (steps jt, queries it), transposed, a tile to a wave: every wave needs them all, as operands
-          // in two parts, and gets them through LDS while its product with the state runs.
+      const float* v_ = lds.v + 4 * hh * lds.VPITCH + 32 * wave + cl;
+      if (OUT) {
+        const float* q_ = lds.q + cl * lds.PITCH + 4 * hh;
+        const float* k_ = lds.k + cl * lds.PITCH + 4 * hh;
+        // each wave takes its share of the scores' sum over the keys' width
+        la_f32x16 P = {};
 #pragma unroll
-          for (int t = 0; t < 3; ++t) {
-            if (t % VT != wave) continue;
-            const int jt = t >> 1, it = (t + 1) >> 1;
-            la_f32x16 P = {};
-#pragma unroll
-            for (int m = 0; m < 2 * KT; ++m) P = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(jt, m), q_frag(it, m), P, 0, 0, 0);
-            const float* f = lds.fade + 31 + 32 * (it - jt) + cl - 4 * hh;
-#pragma unroll
-            for (int mm = 0; mm < 2; ++mm) {
-              la_f32x8 x;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = P[8 * mm + e] * f[-(16 * mm + 8 * (e / 4) + e % 4)];
-              const la_bf16x8 hi = la_round(x);
-              *(la_bf16x8*)&lds.p[t][mm][0][lane * 16] = hi;
-              *(la_bf16x8*)&lds.p[t][mm][1][lane * 16] = la_rest(x, hi);
-            }
-          }
-          if (new_q) {
-            // O^T = S^T Q^T: the accumulator of the state is an operand as it lies
-#pragma unroll
-            for (int it = 0; it < IT; ++it) O[it] = la_f32x16{};
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-              for (int mm = 0; mm < 2; ++mm) {
-                la_f32x8 x;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = S[kt][8 * mm + e];
-                const la_bf16x8 hi = la_round(x), lo = la_rest(x, hi);
-#pragma unroll
-                for (int it = 0; it < IT; ++it) {
-                  const la_bf16x8 qf = q_frag(it, 2 * kt + mm);
-                  O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, qf, O[it], 0, 0, 0);
-                  O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, qf, O[it], 0, 0, 0);
-                }
-              }
-#pragma unroll
-            for (int it = 0; it < IT; ++it)
-#pragma unroll
-              for (int e = 0; e < 16; ++e) O[it][e] *= row_in[it];
-          }
-          __syncthreads();
-          // O^T += V^T P^T
-#pragma unroll
-          for (int t = 0; t < 3; ++t) {
-            const int jt = t >> 1, it = (t + 1) >> 1;
-#pragma unroll
-            for (int mm = 0; mm < 2; ++mm) {
-              const la_bf16x8 vf = v_frag(2 * jt + mm);
-              O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, *(const la_bf16x8*)&lds.p[t][mm][0][lane * 16], O[it], 0, 0, 0);
-              O[it] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, *(const la_bf16x8*)&lds.p[t][mm][1][lane * 16], O[it], 0, 0, 0);
-            }
-          }
+        for (int i = 0; i < 4 * KT / VT; ++i) {
+          const int m = wave + i * VT;
+          const float4 k4 = *(const float4*)(k_ + 8 * m), q4 = *(const float4*)(q_ + 8 * m);
+          P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.x, q4.x, P, 0, 0, 0);
+          P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.y, q4.y, P, 0, 0, 0);
+          P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.z, q4.z, P, 0, 0, 0);
+          P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.w, q4.w, P, 0, 0, 0);
         }
-        // S = lambda^n S + K^T V'
-        if (R.gk > 1 ? st == 0 : last) {
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) lds.p[wave][jj][lane] = la_f32x4{P[4 * jj], P[4 * jj + 1], P[4 * jj + 2], P[4 * jj + 3]};
+        if (new_q) {
+          O = la_f32x16{};
 #pragma unroll
           for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) S[kt][e] *= keep;
-        }
-        if (R.gk > 1 || last) {
-#pragma unroll
-          for (int mb = 0; mb < 4; ++mb) {
-            const la_f32x8 v8 = __builtin_convertvector(v_frag(mb), la_f32x8);
-            const float4 w0 = *(const float4*)&lds.weight[16 * mb + 4 * hh], w1 = *(const float4*)&lds.weight[16 * mb + 8 + 4 * hh];
-            la_f32x8 x = {v8[0] * w0.x, v8[1] * w0.y, v8[2] * w0.z, v8[3] * w0.w, v8[4] * w1.x, v8[5] * w1.y, v8[6] * w1.z, v8[7] * w1.w};
-            for (int part = 0; part < R.parts; ++part) {
-              const la_bf16x8 h = la_round(x);
-#pragma unroll
-              for (int kt = 0; kt < KT; ++kt) {
-                S[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kt_frag(kt, mb), h, S[kt], 0, 0, 0);
-              }
-              x -= __builtin_convertvector(h, la_f32x8);
+            for (int jj = 0; jj < 4; ++jj) {
+              const float4 q4 = *(const float4*)(q_ + 32 * kt + 8 * jj);
+              O = __builtin_amdgcn_mfma_f32_32x32x2f32(S[kt][4 * jj], q4.x, O, 0, 0, 0);
+              O = __builtin_amdgcn_mfma_f32_32x32x2f32(S[kt][4 * jj + 1], q4.y, O, 0, 0, 0);
+              O = __builtin_amdgcn_mfma_f32_32x32x2f32(S[kt][4 * jj + 2], q4.z, O, 0, 0, 0);
+              O = __builtin_amdgcn_mfma_f32_32x32x2f32(S[kt][4 * jj + 3], q4.w, O, 0, 0, 0);
             }
-          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) O[e] *= row_in;
         }
-      } else {
-        const float* v_ = lds.v + 4 * hh * lds.VPITCH + 32 * wave + cl;
-        if (OUT) {
-          const float* q_ = lds.q + cl * lds.PITCH + 4 * hh;
-          const float* k_ = lds.k + cl * lds.PITCH + 4 * hh;
-          // each wave takes its share of the scores' sum over the keys' width
-          la_f32x16 P = {};
+        __syncthreads();
+        const float* f = lds.fade + 31 + cl - 4 * hh;
 #pragma unroll
-          for (int i = 0; i < 4 * KT / VT; ++i) {
-            const int m = wave + i * VT;
-            const float4 k4 = *(const float4*)(k_ + 8 * m), q4 = *(const float4*)(q_ + 8 * m);
-            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.x, q4.x, P, 0, 0, 0);
-            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.y, q4.y, P, 0, 0, 0);
-            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.z, q4.z, P, 0, 0, 0);
-            P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.w, q4.w, P, 0, 0, 0);
-          }
+        for (int jj = 0; jj < 4; ++jj) {
+          la_f32x4 x = lds.p[0][jj][lane];
 #pragma unroll
-          for (int jj = 0; jj < 4; ++jj) lds.p[wave][jj][lane] = la_f32x4{P[4 * jj], P[4 * jj + 1], P[4 * jj + 2], P[4 * jj + 3]};
-          if (new_q) {
-            O[0] = la_f32x16{};
+          for (int w = 1; w < VT; ++w) x += lds.p[w][jj][lane];
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-              for (int jj = 0; jj < 4; ++jj) {
-                const float4 q4 = *(const float4*)(q_ + 32 * kt + 8 * jj);
-                O[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(S[kt][4 * jj], q4.x, O[0], 0, 0, 0);
-                O[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(S[kt][4 * jj + 1], q4.y, O[0], 0, 0, 0);
-                O[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(S[kt][4 * jj + 2], q4.z, O[0], 0, 0, 0);
-                O[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(S[kt][4 * jj + 3], q4.w, O[0], 0, 0, 0);
-              }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) O[0][e] *= row_in[0];
-          }
-          __syncthreads();
-          const float* f = lds.fade + 31 + cl - 4 * hh;
-#pragma unroll
-          for (int jj = 0; jj < 4; ++jj) {
-            la_f32x4 x = lds.p[0][jj][lane];
-#pragma unroll
-            for (int w = 1; w < VT; ++w) x += lds.p[w][jj][lane];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) P[4 * jj + i] = x[i] * f[-(8 * jj + i)];
-          }
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            O[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v_[(8 * (e / 4) + e % 4) * lds.VPITCH], P[e], O[0], 0, 0, 0);
+          for (int i = 0; i < 4; ++i) P[4 * jj + i] = x[i] * f[-(8 * jj + i)];
         }
-        if (R.gk > 1 ? st == 0 : last) {
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt)
+        for (int e = 0; e < 16; ++e)
+          O = __builtin_amdgcn_mfma_f32_32x32x2f32(v_[(8 * (e / 4) + e % 4) * lds.VPITCH], P[e], O, 0, 0, 0);
+      }
+      if (gk > 1 ? st == 0 : last) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) S[kt][e] *= keep;
-        }
-        if (R.gk > 1 || last) {
-          const float* k_ = lds.k + 4 * hh * lds.PITCH + cl;
+        for (int kt = 0; kt < KT; ++kt) S[kt] *= keep;
+      }
+      if (gk > 1 || last) {
+        const float* k_ = lds.k + 4 * hh * lds.PITCH + cl;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int j = 8 * (e / 4) + e % 4;
-            const float x = v_[j * lds.VPITCH] * lds.weight[j + 4 * hh];
+        for (int e = 0; e < 16; ++e) {
+          const int j = 8 * (e / 4) + e % 4;
+          const float x = v_[j * lds.VPITCH] * lds.weight[j + 4 * hh];
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) S[kt] = __builtin_amdgcn_mfma_f32_32x32x2f32(k_[j * lds.PITCH + 32 * kt], x, S[kt], 0, 0, 0);
-          }
+          for (int kt = 0; kt < KT; ++kt) S[kt] = __builtin_amdgcn_mfma_f32_32x32x2f32(k_[j * lds.PITCH + 32 * kt], x, S[kt], 0, 0, 0);
         }
       }
 
-      if (OUT && (R.gq > 1 || last)) {
-        // element e = 4 jj + i of tile it is (value 32 wave + 8 jj + 4 hh + i, step 32 it + cl)
-        const __amdgpu_buffer_rsrc_t buf = la_buffer(la_block<T>(R.o, row, R.back, q_head(st)));
-        const unsigned ld = (unsigned)R.o.ld;
+      if (OUT && (gq > 1 || last)) {
+        // element e = 4 jj + i is (value 32 wave + 8 jj + 4 hh + i, step cl)
+        const LaBlock<float> o = la_block<float>(R.o, row, R.back, n, q_head(st));
+        const unsigned at = la_lane<float>(R.o, R.back, cl, 0) + o.at0;
 #pragma unroll
-        for (int it = 0; it < IT; ++it) {
-          const int pos = 32 * it + cl;
-          const unsigned off = ((unsigned)(R.back ? C - 1 - pos : pos) * ld + 32 * wave + 4 * hh) * (unsigned)sizeof(T);
+        for (int jj = 0; jj < 4; ++jj) {
+          const int c0 = 32 * wave + 8 * jj + 4 * hh;
+          if (VEC) {
+            const la_f32x4 y = {O[4 * jj], O[4 * jj + 1], O[4 * jj + 2], O[4 * jj + 3]};
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(la_u32x4, y), o.buf, c0 < dv ? at + 4 * c0 : LA_NOWHERE, 0, 0);
+          } else {
 #pragma unroll
-          for (int jj = 0; jj < 4; ++jj) {
-            const int c0 = 32 * wave + 8 * jj + 4 * hh;
-            const la_f32x4 y = {O[it][4 * jj], O[it][4 * jj + 1], O[it][4 * jj + 2], O[it][4 * jj + 3]};
-            if (VEC) {
-              const unsigned at = pos < n && c0 < R.dv ? off : LA_NOWHERE;
-              if constexpr (F32) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(la_u32x4, y), buf, at, 32 * jj, 0);
-              else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(la_u32x2, __builtin_convertvector(y, la_bf16x4)), buf, at, 16 * jj, 0);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const unsigned at = pos < n && c0 + i < R.dv ? off : LA_NOWHERE;
-                if constexpr (F32) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(y[i]), buf, at, 32 * jj + 4 * i, 0);
-                else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(short, (__bf16)y[i]), buf, at, 16 * jj + 2 * i, 0);
-              }
-            }
+            for (int i = 0; i < 4; ++i)
+              __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(O[4 * jj + i]), o.buf, c0 + i < dv ? at + 4 * (c0 + i) : LA_NOWHERE, 0, 0);
           }
         }
       }
     }
   }
 
-  float* dst = !OUT ? R.seg + seg_at : R.end && s.index == s.count - 1 ? R.end + state_at : nullptr;
+  float* dst = la_state_out(R, w, OUT);
   if (dst) {
     const __amdgpu_buffer_rsrc_t buf = la_buffer(dst);
     int key0 = 4 * hh, col0 = col;
@@ -644,8 +852,8 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_kernel(
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int key = 32 * kt + 8 * (e / 4) + e % 4;
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[kt][e]), buf, key + key0 < R.dk && col0 < R.dv ? state_off : LA_NOWHERE,
-                                              key * R.st_r * 4, 0);
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[kt][e]), buf, ((key + key0 < dk) & (col0 < dv)) ? state_off : LA_NOWHERE,
+                                              key * st_r * 4, 0);
       }
   }
 }
