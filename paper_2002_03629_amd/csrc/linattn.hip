@@ -12,7 +12,7 @@ using namespace jm;
 
 namespace {
 
-constexpr int SPLIT_TARGET = 512;      // workgroups that fill the device: two to a compute unit
+constexpr int UNITS = 256;      // compute units of the device
 
 int block_rows(const linattn_config& c) { return c.dtype == MADE_BF16 ? LA_BF16_ROWS : LA_F32_ROWS; }
 
@@ -43,30 +43,42 @@ struct Split {
   bool on;
 };
 
+int tiles(int d) { return d <= 32 ? 1 : d <= 64 ? 2 : 4; }
+
 // One workgroup for each head of a sequence, unless those fill less than the device: then the sequences are cut into
-// segments, whose sums and entering states take another pass over keys and values and two more launches.
-Split choose(const linattn_config& c, int roles) {
+// segments, whose sums and entering states take a second pass over keys and values and two more launches.  The number of
+// blocks to a segment is the one with the least time by what was measured (us, widths of 128, bf16 / fp32): a block of the
+// walk 4.4 / 6.8 on a compute unit of its own and 3.2 / 5 more for each further head that shares the state, 1.7 times that
+// where two workgroups share the unit; a block of the pass for the sums 1.9 / 2.9; 4 and 2 to begin; the states in memory
+// three times; 8 for the launches.  32768 steps of 32 heads: whole 2260 us, cut in 16 405; 16 x 1024 of 16: 77 and 110.
+Split choose(const linattn_config& c, bool backward) {
   const int C = block_rows(c);
   const long long blocks = ((long long)c.T + C - 1) / C;     // of the longest sequence there may be
-  const long long units = (long long)c.kv_heads * roles;
-  const long long seqs = c.B;
   const int whole_rows = (int)std::min<long long>(std::max<long long>(blocks, 1) * C, 0x7fffffff / C * C);
-  Split whole = {whole_rows, c.B, false};
-  if (blocks <= 1) return whole;
-  auto slots = [&](long long L) { return c.offsets ? blocks / L + seqs : (blocks + L - 1) / L * seqs; };
-  auto rounds = [&](long long n) { return (double)std::max<long long>(1, (n * units + SPLIT_TARGET - 1) / SPLIT_TARGET); };
-  double best = rounds(seqs) * (blocks + 2);
-  long long best_l = blocks;
-  for (long long L = 1; L < blocks; L = L < 8 ? L + 1 : L + L / 4) {
-    const double cost = rounds(slots(L)) * (1.5 * L + 5) + 0.3 * blocks / L + 8;
-    if (cost < best) {
-      best = cost;
-      best_l = L;
+  Split best = {whole_rows, c.B, false};
+  const int group = c.heads / c.kv_heads;
+  const double size = (c.dtype == MADE_BF16 ? 1.0 : 1.55) * (0.55 + 0.45 * tiles(c.Dk) * tiles(c.Dv) / 16.0);
+  const double walk = size * (4.4 + 3.2 * (group - 1)), sums = size * 1.9 * (backward ? 0.5 * (1 + group) : 1.0);
+  const double heads = (double)c.kv_heads;
+  auto turns = [](double n) { return n <= UNITS ? 1.0 : 1.7 * std::ceil(n / (2 * UNITS)); };
+  double least = turns(c.B * heads * (backward ? 3 : 1)) * (walk * (double)blocks + 4.0);
+  long long last = blocks;
+  for (long long m = 2; m <= blocks && m <= 4096; ++m) {
+    const long long L = (blocks + m - 1) / m;
+    if (L == last) continue;
+    last = L;
+    const double slots = c.offsets ? (double)(blocks / L + c.B) : (double)((blocks + L - 1) / L) * c.B;
+    const double states = slots * heads * c.Dk * c.Dv * 4.0 * (backward ? 2 : 1);
+    const double cost = turns(slots * heads * (backward ? 3 : 1)) * (walk * (double)L + 4.0) +
+                        turns(slots * heads * (backward ? 2 : 1)) * (sums * (double)L + 2.0) + states * 3.0 / 5e6 + 8.0;
+    if (cost < least && slots < 1e9) {
+      least = cost;
+      best.rows = (int)(L * C);
+      best.slots = (int)slots;
+      best.on = true;
     }
   }
-  if (best_l >= blocks) return whole;
-  Split s = {(int)(best_l * C), (int)slots(best_l), true};
-  return s;
+  return best;
 }
 
 long long state_floats(const linattn_config& c, const Split& s) { return s.on ? (long long)s.slots * c.kv_heads * c.Dk * c.Dv : 0; }
@@ -84,8 +96,6 @@ bool pieces(const LinattnView& v, int dtype) {
   const int size = dtype == MADE_BF16 ? 2 : 4;
   return !v.p || ((uintptr_t)v.p % 16 == 0 && v.ld * size % 16 == 0 && v.dim * size % 16 == 0);
 }
-
-int tiles(int d) { return d <= 32 ? 1 : d <= 64 ? 2 : 4; }
 
 template <typename T, int KT, int VT, bool OUT, bool VEC>
 void launch_walk(const LinattnArgs& a, hipStream_t s) {
@@ -165,7 +175,7 @@ int check_grid(const char* who, const linattn_config& c, const Split& s, int rol
 extern "C" int linattn_workspace_bytes(const linattn_config* cfg, int32_t backward, int64_t* bytes) {
   if (!bytes) return fail(MADE_ERR_ARG, "linattn_workspace_bytes: NULL argument");
   TRY(check("linattn_workspace_bytes", cfg, false));
-  *bytes = state_floats(*cfg, choose(*cfg, backward ? 3 : 1)) * 4 * (backward ? 2 : 1);
+  *bytes = state_floats(*cfg, choose(*cfg, backward != 0)) * 4 * (backward ? 2 : 1);
   return MADE_OK;
 }
 
@@ -177,7 +187,7 @@ extern "C" int linattn_forward(const linattn_config* cfg, const void* q, const v
   const linattn_config& c = *cfg;
   if (c.B == 0) return MADE_OK;
   if (!log_decay || (c.T > 0 && (!q || !k || !v || !o))) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
-  Split split = choose(c, 1);
+  Split split = choose(c, false);
   TRY(take_workspace(who, c, workspace, workspace_bytes, 1, split));
   TRY(check_grid(who, c, split, 1));
   hipStream_t s = (hipStream_t)stream;
@@ -218,7 +228,7 @@ extern "C" int linattn_backward(const linattn_config* cfg, const void* q, const 
   if (c.B == 0) return MADE_OK;
   if (!log_decay || (c.T > 0 && (!q || !k || !v || !d_o || !dq || !dk || !dv))) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
   if (d_state_in && d_state_in == d_state_out) return fail(MADE_ERR_ARG, "%s: d_state_in is d_state_out", who);
-  Split split = choose(c, 3);
+  Split split = choose(c, true);
   TRY(take_workspace(who, c, workspace, workspace_bytes, 2, split));
   TRY(check_grid(who, c, split, 3));
   hipStream_t s = (hipStream_t)stream;
@@ -321,7 +331,7 @@ extern "C" int linattn_step(const linattn_config* cfg, const void* q, const void
   a.vec = (uintptr_t)state % 16 == 0 && c.Dv % 4 == 0;
   const long long units = (long long)c.B * c.kv_heads;
   // whole rows of the state (512 bytes) in one workgroup where there are enough of them to fill the device
-  const bool wide = units >= SPLIT_TARGET && c.Dv > 32;
+  const bool wide = units >= 2 * UNITS && c.Dv > 32;
   const long long grid = units * (wide ? (c.Dv + 127) / 128 : (c.Dv + 31) / 32);
   if (grid > 0x7fffffffLL) return fail(MADE_ERR_ARG, "%s: B=%d, heads=%d are more than one launch takes", who, c.B, c.kv_heads);
   hipStream_t s = (hipStream_t)stream;

@@ -69,6 +69,11 @@ __device__ __forceinline__ float la_pow(float g2, int n) {
   return n == 0 ? 1.0f : x;
 }
 
+// The same value in every lane, as a scalar.
+__device__ __forceinline__ float la_uniform(float x) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+
 // ------------------------------------------------------------------------------------------------------------------
 // segments
 // ------------------------------------------------------------------------------------------------------------------
@@ -230,7 +235,7 @@ __device__ __forceinline__ bool la_place(const LinattnArgs& a, bool out, Linattn
   w.first = R.back ? row + s.len - 1 : row;
   w.state_at = ((long long)s.b * a.kv_heads + w.head) * R.dk * R.dv;
   w.seg_at = ((long long)slot * a.kv_heads + w.head) * R.dk * R.dv;
-  w.g2 = a.log_decay[w.head] * 1.44269504088896340736f;
+  w.g2 = la_uniform(a.log_decay[w.head] * 1.44269504088896340736f);
   return true;
 }
 
@@ -241,9 +246,10 @@ __device__ __forceinline__ float* la_state_out(const LinattnRole& R, const Linat
   return !out ? R.seg + w.seg_at : R.end && w.s.index == w.s.count - 1 ? R.end + w.state_at : nullptr;
 }
 
-// A value the compiler cannot know to be the one it has already.
-__device__ __forceinline__ int la_again(int x) {
-  asm volatile("" : "+v"(x));
+// The lane's number, formed anew: what is made of it need not be kept from one use to the next.
+__device__ __forceinline__ int la_lane_id() {
+  int x;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
   return x;
 }
 
@@ -268,14 +274,14 @@ __device__ __forceinline__ la_u32x4 la_rest(la_f32x8 x, la_u32x4 hi) { return la
 // k = 8 (l / 16) ..  Two accumulators above each other are so an operand with 32 values of k in the order of quads
 // 0 4 1 5 2 6 3 7: the state and the scores become operands as they lie, and what they are multiplied with is laid out in
 // that order: q and k by rows (dims), k and v by columns (steps).
-constexpr int LA_FADE = 16;     // place of the factor lambda^0 in the table
+constexpr int LA_FADE = 32;     // place of the factor lambda^0 in the table
 
 template <int KT, int VT, bool OUT>
 struct LaLds {
-  static constexpr int PITCH = KT * 32 * 2 + 16;                 // bytes from row to row: 16 rows in 64 banks
-  __align__(16) unsigned char q[OUT ? 64 * PITCH : 16];
-  __align__(16) unsigned char k[OUT ? 64 * PITCH : 16];
-  // 16-byte units of a column are exchanged (la_swizzle): neither writes by rows nor reads by columns meet in a bank
+  // 16-byte units of a row and of a column are exchanged (la_row_swizzle, la_swizzle) so that the 16 rows or columns an
+  // operand is read from lie in different banks
+  __align__(16) unsigned char q[OUT ? 64 * KT * 64 : 16];
+  __align__(16) unsigned char k[OUT ? 64 * KT * 64 : 16];
   __align__(16) unsigned char kt[KT * 32 * 128];
   __align__(16) unsigned char vt[VT * 32 * 128];
   __align__(16) unsigned char p[OUT ? 6 : 1][2][64 * 16];        // scores as operands: pair of tiles, part, lane
@@ -284,7 +290,12 @@ struct LaLds {
 };
 
 __device__ __forceinline__ int la_swizzle(int d) { return ((d >> 1) ^ (d >> 4)) & 7; }
-__device__ __forceinline__ int la_quad(int q) { return (q & 3) * 2 + (q >> 2 & 1); }       // place of quad q of 8
+template <int KT>
+__device__ __forceinline__ int la_row_swizzle(int row) {
+  return KT == 4 ? row & 15 : KT == 2 ? row >> 1 & 7 : row >> 2 & 3;
+}
+// The group of rows a lane takes: neighbours take both halves of a column's unit.
+__device__ __forceinline__ int la_group(int m) { return (m & 8) | (m & 1) << 2 | (m >> 1 & 3); }
 
 __device__ __forceinline__ uint32_t la_pack(float x, float y) {
   typedef __attribute__((ext_vector_type(2))) __bf16 pair;
@@ -292,19 +303,16 @@ __device__ __forceinline__ uint32_t la_pack(float x, float y) {
   return __builtin_bit_cast(uint32_t, h);
 }
 
-// place of the scores of queries 16 it .. and steps 32 kb .. (the second halves of 0 and 3 lie above the diagonal)
+// place of the scores of queries 16 it .. and steps 32 kb ..
 __device__ __forceinline__ constexpr int la_pair(int it, int kb) { return it < 2 ? it : 2 * it - 2 + kb; }
 
-// rows p .. p + rows - 1, piece u
-__device__ __forceinline__ void la_put_rows(const la_u32x4* r, int rows, unsigned char* dst, int pitch, int p, int u) {
-  unsigned char* at = dst + p * pitch + (u >> 2) * 64 + la_quad(2 * u & 7) * 8;            // (quad 2 u + 1 lies two places on)
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (e < rows) {
-      *(la_u32x2*)(at + e * pitch) = la_u32x2{r[e][0], r[e][1]};
-      *(la_u32x2*)(at + e * pitch + 16) = la_u32x2{r[e][2], r[e][3]};
-    }
-  }
+// row p, piece u: its two quads are the same halves of two neighbouring units
+template <int KT>
+__device__ __forceinline__ void la_put_row(la_u32x4 r, unsigned char* dst, int p, int u) {
+  unsigned char* row = dst + p * (KT * 64) + (u >> 1 & 1) * 8;
+  const int unit = ((u >> 2) * 4 + (u & 1) * 2) ^ la_row_swizzle<KT>(p);
+  *(la_u32x2*)(row + unit * 16) = la_u32x2{r[0], r[1]};
+  *(la_u32x2*)(row + (unit ^ 1) * 16) = la_u32x2{r[2], r[3]};
 }
 
 // rows 4 tg .. 4 tg + 3, piece u, turned over
@@ -323,11 +331,12 @@ __device__ __forceinline__ void la_put_columns(const la_u32x4 (&r)[4], unsigned 
 }
 
 template <int TILES, int NT>
-__device__ __forceinline__ void la_fetch_rows(const LinattnView& x, long long first, int back, int n, int head, unsigned char* dst, int pitch) {
+__device__ __forceinline__ void la_fetch_rows(const LinattnView& x, long long first, int back, int n, int head, unsigned char* dst) {
 #pragma unroll 4
   for (int i = threadIdx.x; i < 64 * 32 * TILES; i += NT) {
     const int pos = i / (32 * TILES), d = i % (32 * TILES);
-    *(la_bf16*)(dst + pos * pitch + (d >> 5) * 64 + la_quad(d >> 2 & 7) * 8 + (d & 3) * 2) = la_element<la_bf16>(x, first, back, n, head, pos, d);
+    *(la_bf16*)(dst + pos * (TILES * 64) + (((d >> 5) * 4 + (d >> 2 & 3)) ^ la_row_swizzle<TILES>(pos)) * 16 + (d >> 4 & 1) * 8 + (d & 3) * 2) =
+        la_element<la_bf16>(x, first, back, n, head, pos, d);
   }
 }
 
@@ -363,7 +372,7 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
   // ---- state: element e of tile t is (key 16 t + 4 g + e, value 16 wave + cl)
   la_f32x4 S[2 * KT];
   const int col = 16 * wave + cl;
-  unsigned state_off = (unsigned)(4 * g * R.st_r + col * R.st_c) * 4;
+  const unsigned state_off = (unsigned)(4 * g * R.st_r + col * R.st_c) * 4;
   if (OUT) {
     const float* src = la_state_in(R, w);
     const __amdgpu_buffer_rsrc_t buf = la_buffer(src);
@@ -382,8 +391,6 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
 
   if (OUT) {
     for (int i = threadIdx.x; i < LA_FADE + 64; i += NT) lds.fade[i] = i < LA_FADE ? 0.0f : R.p_scale * la_pow(g2, i - LA_FADE);
-    // (tiles above the diagonal: the second halves of pairs 0 and 3)
-    for (int i = threadIdx.x; i < 4 * 64; i += NT) *(la_u32x2*)&lds.p[(i >> 7) * 3][i >> 6 & 1][(i & 63) * 16 + 8] = la_u32x2{};
   }
 
   const int stages = gq > gk ? gq : gk;
@@ -401,7 +408,7 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
     const bool keys = part < KT;
     const int at = (keys ? part : part - KT) * 64 + lane, U = keys ? 4 * KT : 4 * VT;
     const LinattnView x = keys ? R.k : R.v;
-    kv_lane[i] = part < KT + VT ? la_lane<la_bf16>(x, R.back, at / U * 4, at % U * 8) : LA_NOWHERE;
+    kv_lane[i] = part < KT + VT ? la_lane<la_bf16>(x, R.back, la_group(at / U) * 4, at % U * 8) : LA_NOWHERE;
   }
 #pragma unroll
   for (int i = 0; i < PERQ; ++i) {
@@ -432,21 +439,23 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
   la_f32x4 O[4];
   for (int p = w.p0; p < w.p1; p += C) {
     const int n = min(C, w.p1 - p);
-    float next = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(frame * la_pow(g2, n))));
-    const bool rescale = !(next >= 0x1p-30f && next <= 0x1p30f);
-    const float factor = next;
-    next = rescale ? 1.0f : next;
+    const float factor = la_uniform(frame * la_pow(g2, n));
+    const bool rescale = __builtin_amdgcn_readfirstlane(!(factor >= 0x1p-30f && factor <= 0x1p30f));
+    const float next = la_uniform(rescale ? 1.0f : factor);
     const long long row = R.back ? w.first - p : w.first + p;
     for (int st = 0; st < stages; ++st) {
       const bool new_q = gq > 1 || st == 0, new_kv = gk > 1 || st == 0, last = st == stages - 1;
       __syncthreads();                       // every wave has read the block before
       if (VEC) {
-        const int lane = la_again(threadIdx.x & 63);
+        const int lane = la_lane_id();
         if (OUT && new_q) {
 #pragma unroll
           for (int i = 0; i < PERQ; ++i) {
             const int at = 64 * wave + lane + i * NT;
-            if (at < 128 * KT) la_put_rows(qs[i], 2, lds.q, lds.PITCH, at / (4 * KT) * 2, at % (4 * KT));
+            if (at < 128 * KT) {
+#pragma unroll
+              for (int e = 0; e < 2; ++e) la_put_row<KT>(qs[i][e], lds.q, at / (4 * KT) * 2 + e, at % (4 * KT));
+            }
           }
         }
         if (new_kv) {
@@ -454,25 +463,28 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
           for (int i = 0; i < PER; ++i) {
             const int part = wave + i * NW;
             if (part < KT) {
-              const int at = part * 64 + lane, tg = at / (4 * KT), u = at % (4 * KT);
-              if (OUT) la_put_rows(kv[i], 4, lds.k, lds.PITCH, 4 * tg, u);
+              const int at = part * 64 + lane, tg = la_group(at / (4 * KT)), u = at % (4 * KT);
+              if (OUT) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) la_put_row<KT>(kv[i][e], lds.k, 4 * tg + e, u);
+              }
               la_put_columns(kv[i], lds.kt, tg, u);
             } else if (part < KT + VT) {
               const int at = (part - KT) * 64 + lane;
-              la_put_columns(kv[i], lds.vt, at / (4 * VT), at % (4 * VT));
+              la_put_columns(kv[i], lds.vt, la_group(at / (4 * VT)), at % (4 * VT));
             }
           }
         }
       } else {
-        if (OUT && new_q) la_fetch_rows<KT, NT>(R.q, row, R.back, n, q_head(st), lds.q, lds.PITCH);
+        if (OUT && new_q) la_fetch_rows<KT, NT>(R.q, row, R.back, n, q_head(st), lds.q);
         if (new_kv) {
-          if (OUT) la_fetch_rows<KT, NT>(R.k, row, R.back, n, k_head(st), lds.k, lds.PITCH);
+          if (OUT) la_fetch_rows<KT, NT>(R.k, row, R.back, n, k_head(st), lds.k);
           la_fetch_columns<KT, NT>(R.k, row, R.back, n, k_head(st), lds.kt);
           la_fetch_columns<VT, NT>(R.v, row, R.back, n, k_head(st), lds.vt);
         }
       }
       if (new_kv && wave == 0) {
-        const int j = la_again(threadIdx.x & 63);
+        const int j = la_lane_id();
         lds.weight[j] = R.s_scale / next * la_pow(g2, max(0, n - 1 + late - j));
       }
       if (VEC) request(last ? p + C : p, last ? 0 : st + 1);
@@ -481,42 +493,42 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
       // (what a lane's number makes of addresses is formed again for every product: kept, it would take the registers that
       // let four waves share a SIMD)
       if (OUT) {
-        {
-        const int lane = la_again(threadIdx.x & 63), cl = lane & 15, g = lane >> 4;
-        const unsigned char* q_ = lds.q + cl * lds.PITCH + g * 16;
-        const unsigned char* k_ = lds.k + cl * lds.PITCH + g * 16;
-        // Scores of the 10 tiles (steps jt <= queries it), transposed, divided among the waves: every wave needs them all, as
-        // operands in two parts, and gets them through LDS while its product with the state runs.
-        for (int t = wave; t < 10; t += NW) {
-          const int it = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, jt = t - it * (it + 1) / 2;
-          const unsigned char* qt = q_ + it * 16 * lds.PITCH;
-          const unsigned char* kr = k_ + jt * 16 * lds.PITCH;
-          la_f32x4 P = {};
-          la_u32x4 qf[KT], kf[KT];
+        // Scores of the 6 pairs of tiles with steps <= queries, transposed, divided among the waves: every wave needs them all,
+        // as operands in two parts, and gets them through LDS while its product with the state runs.
+        for (int pair = wave; pair < 6; pair += NW) {
+          const int it = pair < 2 ? pair : pair / 2 + 1, kb0 = pair == 3 || pair == 5;
+          const int lane = la_lane_id(), cl = lane & 15, g = lane >> 4;
+          const int sw = la_row_swizzle<KT>(cl);
+          const unsigned char* q_ = lds.q + (16 * it + cl) * (KT * 64);
+          const unsigned char* k_ = lds.k + (32 * kb0 + cl) * (KT * 64);
+          la_u32x4 qf[KT], kf[2][KT];
 #pragma unroll
           for (int kb = 0; kb < KT; ++kb) {
-            qf[kb] = *(const la_u32x4*)(qt + kb * 64);
-            kf[kb] = *(const la_u32x4*)(kr + kb * 64);
+            const int unit = ((4 * kb + g) ^ sw) * 16;
+            qf[kb] = *(const la_u32x4*)(q_ + unit);
+            kf[0][kb] = *(const la_u32x4*)(k_ + unit);
+            kf[1][kb] = *(const la_u32x4*)(k_ + unit + 16 * KT * 64);
           }
           __builtin_amdgcn_sched_barrier(0);      // (all requested before the first is waited for)
+          la_f32x4 P[2] = {};
 #pragma unroll
-          for (int kb = 0; kb < KT; ++kb) P = la_mfma16(kf[kb], qf[kb], P);
-          const float* f = lds.fade + LA_FADE + 16 * (it - jt) + cl - 4 * g;
-          uint32_t hi[2], lo[2];
+          for (int kb = 0; kb < KT; ++kb)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float x = P[2 * e] * f[-2 * e], y = P[2 * e + 1] * f[-2 * e - 1];
-            hi[e] = la_pack(x, y);
-            lo[e] = la_pack(x - __uint_as_float(hi[e] << 16), y - __uint_as_float(hi[e] & 0xffff0000u));
-          }
-          *(la_u32x2*)&lds.p[la_pair(it, jt >> 1)][0][lane * 16 + (jt & 1) * 8] = la_u32x2{hi[0], hi[1]};
-          *(la_u32x2*)&lds.p[la_pair(it, jt >> 1)][1][lane * 16 + (jt & 1) * 8] = la_u32x2{lo[0], lo[1]};
-        }
+            for (int t = 0; t < 2; ++t) P[t] = la_mfma16(kf[t][kb], qf[kb], P[t]);
+          const float* f = lds.fade + LA_FADE + 16 * (it - 2 * kb0) + cl - 4 * g;
+          la_f32x8 x;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = P[e / 4][e % 4] * f[-(16 * (e / 4) + e % 4)];
+          const la_u32x4 hi = la_round(x);
+          *(la_u32x4*)&lds.p[pair][0][lane * 16] = hi;
+          *(la_u32x4*)&lds.p[pair][1][lane * 16] = la_rest(x, hi);
         }
         if (new_q) {
-          const int lane = la_again(threadIdx.x & 63);
-          const unsigned char* q_ = lds.q + (lane & 15) * lds.PITCH + (lane >> 4) * 16;
-          auto q_frag = [&](int it, int kb) { return *(const la_u32x4*)(q_ + it * 16 * lds.PITCH + kb * 64); };
+          const int lane = la_lane_id();
+          // (la_row_swizzle(16 it + c) = la_row_swizzle(c))
+          const unsigned char* q_ = lds.q + (lane & 15) * (KT * 64);
+          const int qsw = ((lane >> 4) ^ la_row_swizzle<KT>(lane & 15)) * 16;
+          auto q_frag = [&](int it, int kb) { return *(const la_u32x4*)(q_ + (qsw ^ 64 * kb) + it * 16 * KT * 64); };
           // O^T = S^T Q^T: the accumulator of the state is an operand as it lies
           la_u32x4 qf[2][4];
 #pragma unroll
@@ -547,7 +559,7 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
         }
         __syncthreads();
       }
-      const int lane = la_again(threadIdx.x & 63), cl = lane & 15, g = lane >> 4;
+      const int lane = la_lane_id(), cl = lane & 15, g = lane >> 4;
       // (la_swizzle(16 t + c) = la_swizzle(c) ^ t for c < 16)
       const unsigned char* kt_ = lds.kt + cl * 128;
       const unsigned char* vt_ = lds.vt + (16 * wave + cl) * 128;
@@ -620,8 +632,8 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
   float* dst = la_state_out(R, w, OUT);
   if (dst) {
     const __amdgpu_buffer_rsrc_t buf = la_buffer(dst);
-    int key0 = 4 * g, col0 = col;
-    asm volatile("" : "+v"(state_off), "+v"(key0), "+v"(col0));      // (formed again, not kept from the loads)
+    const int lane = la_lane_id(), key0 = 4 * (lane >> 4), col0 = 16 * wave + (lane & 15);      // (not kept from the loads)
+    const unsigned state_off = (unsigned)(key0 * st_r + col0 * R.st_c) * 4;
 #pragma unroll
     for (int t = 0; t < 2 * KT; ++t)
 #pragma unroll
