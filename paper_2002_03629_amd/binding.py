@@ -23,6 +23,7 @@ EXPORTS = ["made_init", "made_conv_init", "made_free", "made_forward_logits", "m
            "made_layer_nnz",
            "rnn_forward", "rnn_backward_sequential", "rnn_backward_jacobi", "rnn_jacobi_max_steps", "rnn_param_grads",
            "linattn_workspace_bytes", "linattn_forward", "linattn_backward", "linattn_step",
+           "adamw_step", "adamw_unpack",
            "made_last_error"]
 
 
@@ -47,6 +48,14 @@ class linattn_config(C.Structure):
                 ("Dv", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("ld_q", C.c_int64), ("ld_k", C.c_int64),
                 ("ld_v", C.c_int64), ("ld_o", C.c_int64), ("offsets", C.c_void_p)]
 
+
+class adamw_config(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("grad_scale", C.c_double), ("step", C.c_int32), ("param_dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("moment_bits", C.c_int32)]
+
+
+ADAMW_BLOCK = 256
 
 _lib = None
 
@@ -94,6 +103,9 @@ def lib() -> C.CDLL:
         L.linattn_forward.argtypes = [cfg] + [vp] * 8 + [C.c_int64, vp]
         L.linattn_backward.argtypes = [cfg] + [vp] * 12 + [C.c_int64, vp]
         L.linattn_step.argtypes = [cfg] + [vp] * 5 + [i32, vp, vp, vp]
+        vpp = C.POINTER(vp)
+        L.adamw_step.argtypes = [C.POINTER(adamw_config), i32, i64p] + [vpp] * 7 + [vp, vp]
+        L.adamw_unpack.argtypes = [i32, i64p] + [vpp] * 6 + [vp]
         L.made_last_error.argtypes = []
         L.made_last_error.restype = C.c_char_p
         for name in EXPORTS[:-1]:
@@ -544,3 +556,99 @@ def linattn_step(q, k, v, log_decay, state, slots, B: int, heads: int, kv_heads:
                  stream=None) -> None:
     """state [n_slots, kv_heads, Dk, Dv] is updated in place; slots: int32 [B] or None (row b has place b)."""
     PreparedLinattnStep(q, k, v, log_decay, state, slots, B, heads, kv_heads, Dk, Dv, scale, o, stream)()
+
+
+# ------------------------------------------------------------------------------------------------
+# AdamW over many tensors (include/jacobi_adamw.h).  Weights and gradients are float32 or bfloat16 (each list of one type),
+# moments float32, or int8 and uint8 with float32 scales (adamw_moments makes zeroed ones).
+# ------------------------------------------------------------------------------------------------
+def adamw_moments(params, bits: int = 32):
+    """Zeroed moments for these tensors: (m, v, m_scale, v_scale), lists; the scales are None for 32 bits."""
+    import torch
+    if bits == 32:
+        return [torch.zeros_like(p, dtype=torch.float32) for p in params], [torch.zeros_like(p, dtype=torch.float32) for p in params], None, None
+    if bits != 8:
+        raise ValueError(f"moments have 8 or 32 bits, not {bits}")
+    scales = [[torch.zeros(-(-p.numel() // ADAMW_BLOCK), dtype=torch.float32, device=p.device) for p in params] for _ in range(2)]
+    return ([torch.zeros_like(p, dtype=torch.int8) for p in params], [torch.zeros_like(p, dtype=torch.uint8) for p in params],
+            scales[0], scales[1])
+
+
+def _pointers(tensors, what: str, dtype, sizes, stream=None):
+    """Host array of the device pointers of contiguous tensors of these sizes and one type."""
+    if len(tensors) != len(sizes):
+        raise ValueError(f"{len(tensors)} tensors in {what}, expected {len(sizes)}")
+    out = (C.c_void_p * len(sizes))()
+    for i, t in enumerate(tensors):
+        _on_device(t, f"{what}[{i}]", stream)
+        if t.numel() != sizes[i]:
+            raise ValueError(f"{what}[{i}] has {t.numel()} elements, expected {sizes[i]}")
+        out[i] = _ptr(t, dtype) or None
+    return out
+
+
+class PreparedAdamW:
+    """adamw_step with its tensors checked and marshalled once, for loops that take step after step on the same buffers (a
+    gradient that is allocated anew for every step needs a new object): calling the object runs a step.  The tensors are kept
+    alive; their contents may change between calls."""
+
+    def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, copies=None):
+        import torch
+        if not params:
+            raise ValueError("no tensors")
+        sizes = [p.numel() for p in params]
+        blocks = [-(-n // ADAMW_BLOCK) for n in sizes]
+        eight = m_scale is not None
+        if eight != (v_scale is not None):
+            raise ValueError("m_scale and v_scale go together")
+        for what, ts in (("params", params), ("grads", grads)):
+            if ts[0].dtype not in (torch.float32, torch.bfloat16):
+                raise ValueError(f"{what}: expected torch.float32 or torch.bfloat16, got {ts[0].dtype}")
+        f = torch.float32
+        self._device = params[0].device
+        self._n = C.c_int32(len(sizes))
+        self._sizes = (C.c_int64 * len(sizes))(*sizes)
+        self._arrays = [_pointers(params, "params", params[0].dtype, sizes), _pointers(grads, "grads", grads[0].dtype, sizes),
+                        _pointers(m, "m", torch.int8 if eight else f, sizes), _pointers(v, "v", torch.uint8 if eight else f, sizes),
+                        _pointers(m_scale, "m_scale", f, blocks) if eight else None,
+                        _pointers(v_scale, "v_scale", f, blocks) if eight else None,
+                        _pointers(copies, "copies", torch.bfloat16, sizes) if copies is not None else None]
+        written = [t for ts in (params, m, v, m_scale, v_scale, copies) if ts is not None for t in ts if t.numel()]
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in written)
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("two of the tensors that are written overlap (is one listed twice?)")
+        self._cfg = adamw_config()
+        self._cfg.param_dtype = MADE_BF16 if params[0].dtype == torch.bfloat16 else MADE_F32
+        self._cfg.grad_dtype = MADE_BF16 if grads[0].dtype == torch.bfloat16 else MADE_F32
+        self._cfg.moment_bits = 8 if eight else 32
+        self._keep = (params, grads, m, v, m_scale, v_scale, copies)
+        self._fn = lib().adamw_step
+
+    def __call__(self, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, step: int, grad_scale: float = 1.0,
+                 scalars=None, stream=None) -> None:
+        """scalars: float64 [4] on the device, {lr, 1 / (1 - beta1^step), 1 / (1 - beta2^step), grad_scale}, read when the step
+        runs in place of lr, step and grad_scale (a recorded step then follows them), or None."""
+        import torch
+        c = self._cfg
+        c.lr, c.beta1, c.beta2, c.eps, c.weight_decay, c.grad_scale, c.step = lr, beta1, beta2, eps, weight_decay, grad_scale, step
+        if self._device.index != (torch.cuda.current_device() if stream is None else stream.device.index):
+            raise ValueError(f"the tensors are on {self._device}, the call is for another device")
+        _check(self._fn(C.byref(c), self._n, self._sizes, *self._arrays, _dense(scalars, "scalars", (4,), torch.float64, stream),
+                        _stream(stream)))
+
+
+def adamw_step(params, grads, m, v, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, step: int, m_scale=None,
+               v_scale=None, copies=None, grad_scale: float = 1.0, scalars=None, stream=None) -> None:
+    PreparedAdamW(params, grads, m, v, m_scale, v_scale, copies)(lr, beta1, beta2, eps, weight_decay, step, grad_scale, scalars, stream)
+
+
+def adamw_unpack(m, v, m_scale, v_scale, m_out, v_out, stream=None) -> None:
+    """The float32 values that 8-bit moments stand for (lists of tensors)."""
+    import torch
+    sizes = [t.numel() for t in m]
+    blocks = [-(-n // ADAMW_BLOCK) for n in sizes]
+    f = torch.float32
+    _check(lib().adamw_unpack(len(sizes), (C.c_int64 * len(sizes))(*sizes), _pointers(m, "m", torch.int8, sizes, stream),
+                              _pointers(v, "v", torch.uint8, sizes, stream), _pointers(m_scale, "m_scale", f, blocks, stream),
+                              _pointers(v_scale, "v_scale", f, blocks, stream), _pointers(m_out, "m_out", f, sizes, stream),
+                              _pointers(v_out, "v_out", f, sizes, stream), _stream(stream)))

@@ -12,7 +12,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libjacobi_made.so")
-SOURCES = ["jacobi_made.hip", "linattn.hip"]
+SOURCES = ["jacobi_made.hip", "linattn.hip", "adamw.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-pthread", "-Wall", "-Wno-unused-function",
     # keep the compiler from forming packed-fp32 instructions

@@ -1,0 +1,311 @@
+"""GPU parity of adamw_step and adamw_unpack (include/jacobi_adamw.h) against oracle/adamw_oracle.py.
+
+Tolerances, element by element, in units of fp32's 2^-24:
+  * 32-bit moments: beta, 1 - beta, two products and a sum: 4 of |beta1 m| + |(1 - beta1) g| (which may cancel), 6 of v;
+  * weights: the factor, the product and the difference: 4 of |p|; the update u = lr c1 m / (sqrt(c2 v) + eps) carries m's error,
+    half of v's and at most 8 roundings of its own: 4 lr c1 (|beta1 m| + |(1 - beta1) g|) / (sqrt(c2 v) + eps) + 11 |u|;
+    bf16 weights and copies: 2^-8 of the value more;
+  * 8-bit moments: computed in 64 bits, so that codes and scales are the oracle's; the update then has 12 |u|."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import adamw_oracle as A
+from oracle import rnn_oracle as R
+from oracle import linattn_oracle as L
+from paper_2002_03629_amd import binding as B
+from paper_2002_03629_amd import synth as S
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+HYPER = dict(lr=3e-3, beta1=0.9, beta2=0.99, eps=1e-7, weight_decay=0.02)
+
+
+def host(t):
+    return t.detach().double().cpu().numpy().reshape(-1)
+
+
+class Tensors:
+    """Tensors of these sizes, each `shift` elements into memory of its own."""
+
+    def __init__(self, sizes, param="f32", grad="f32", bits=32, copies=False, shift=0, seed=0):
+        self.sizes, self.param, self.grad, self.bits = sizes, param, grad, bits
+        self.g = np.random.default_rng(seed)
+        self.shift = shift
+        self.p = [self.make(n, DT[param], 0.05) for n in sizes]
+        self.grads = [self.make(n, DT[grad], 0.0) for n in sizes]
+        mv = B.adamw_moments(self.p, bits)
+        self.m, self.v = ([self.place(t) for t in ts] for ts in mv[:2])
+        self.ms, self.vs = mv[2:]
+        self.copies = [self.place(torch.zeros(n, dtype=torch.bfloat16, device="cuda")) for n in sizes] if copies else None
+
+    def place(self, t):
+        buf = torch.zeros(t.numel() + self.shift, dtype=t.dtype, device="cuda")
+        buf[self.shift:].copy_(t.reshape(-1))
+        return buf[self.shift:]
+
+    def make(self, n, dtype, std):
+        return self.place(torch.from_numpy((self.g.normal(size=n) * std).astype(np.float32)).to(dtype).cuda())
+
+    def new_grads(self, scale=1e-3):
+        for t in self.grads:
+            x = self.g.normal(size=t.numel()) * scale * np.exp(self.g.normal(size=t.numel()))
+            x[self.g.random(t.numel()) < 0.05] = 0.0
+            t.copy_(torch.from_numpy(x.astype(np.float32)).to(t.dtype).cuda())
+
+    def moments(self, i):
+        if self.bits == 32:
+            return host(self.m[i]), host(self.v[i])
+        return A.unpack(host(self.m[i]), host(self.v[i]), host(self.ms[i]), host(self.vs[i]))
+
+    def step(self, t, plan=None, **kw):
+        """a step on the GPU and its comparison with the oracle's from the same values"""
+        h = dict(HYPER)
+        h.update({k: kw.pop(k) for k in list(kw) if k in h})
+        gs = kw.get("grad_scale", 1.0)
+        before = [(host(self.p[i]), host(self.grads[i]), *self.moments(i)) for i in range(len(self.sizes))]
+        plan = plan or B.PreparedAdamW(self.p, self.grads, self.m, self.v, self.ms, self.vs, self.copies)
+        plan(h["lr"], h["beta1"], h["beta2"], h["eps"], h["weight_decay"], t, **kw)
+        torch.cuda.synchronize()
+        self.compare(before, h, t, gs)
+
+    def compare(self, before, h, t, gs):
+        c1, c2 = 1 / (1 - h["beta1"] ** t), 1 / (1 - h["beta2"] ** t)
+        for i, (p0, g0, m0, v0) in enumerate(before):
+            if not len(p0):
+                continue
+            p, m, v = A.step(p0, g0, m0, v0, h["lr"], h["beta1"], h["beta2"], h["eps"], h["weight_decay"], t, gs)
+            mass = np.abs(h["beta1"] * m0) + np.abs((1 - h["beta1"]) * g0 * gs)
+            lever = abs(h["lr"]) * c1 / (np.sqrt(c2 * v) + h["eps"])
+            tol = U * (4 * np.abs(p0) + 12 * lever * np.abs(m) + (4 * lever * mass if self.bits == 32 else 0)) + 1e-44
+            # where v is below fp32's normal numbers its two products are rounded to multiples of 2^-149: v is off by 2^-149 at
+            # most, and u, which has its root below, by half of that over v
+            tol = tol + 0.5 * lever * np.abs(m) * 2.0 ** -149 / np.maximum(v, 2.0 ** -149)
+            got = host(self.p[i])
+            half = 2.0 ** -8 * np.abs(p) if self.param == "bf16" else 0
+            undefined = np.isnan(p) & np.isnan(got)           # (0 / 0: eps of zero and no gradient so far)
+            assert h["eps"] > 0 or (np.isnan(p) == ((v == 0) | np.isnan(p0))).all()
+            assert ((np.abs(got - p) <= tol + half) | undefined).all(), (i, self.sizes[i], np.nanmax(np.abs(got - p)))
+            if self.copies:
+                assert (np.abs(host(self.copies[i]) - p) <= tol + 2.0 ** -8 * np.abs(p)).all(), i
+            if self.bits == 32:
+                assert (np.abs(host(self.m[i]) - m) <= 4 * U * mass + 1e-44).all(), i
+                assert (np.abs(host(self.v[i]) - v) <= 6 * U * v + 3e-45).all(), i
+            else:
+                mc, vc, ms, vs = A.pack(m, v)
+                assert (host(self.ms[i]) == ms).all() and (host(self.vs[i]) == vs).all(), i
+                assert (host(self.m[i]) == mc).all() and (host(self.v[i]) == vc).all(), (i, int((host(self.m[i]) != mc).sum()))
+
+
+SIZES = [1, 3, 255, 256, 257, 0, 4095, 4096, 4097, 13000]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param,grad,copies", [("f32", "f32", False), ("f32", "bf16", True), ("bf16", "bf16", False), ("bf16", "f32", False)])
+def test_steps_from_zero_moments(bits, param, grad, copies):
+    t = Tensors(SIZES, param, grad, bits, copies)
+    for step in range(1, 5):
+        t.new_grads()
+        t.step(step)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_unaligned_tensors(bits, shift):
+    t = Tensors([1000, 5000, 7], "f32", "bf16", bits, True, shift)
+    for step in (1, 2):
+        t.new_grads()
+        t.step(step)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_tensors_than_a_launch_takes(bits):
+    t = Tensors([17 + 37 * (i % 11) for i in range(130)], bits=bits)
+    t.new_grads()
+    t.step(1)
+    t.new_grads()
+    t.step(2)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_large_tensor(bits):
+    t = Tensors([(1 << 22) + 5], "f32", "f32", bits)
+    for step in (1, 2):
+        t.new_grads()
+        t.step(step)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_hyperparameters(bits):
+    for i, kw in enumerate([dict(weight_decay=0.0), dict(beta1=0.0), dict(beta2=0.0, eps=1e-3), dict(lr=0.0), dict(lr=-0.01), dict(grad_scale=0.125)]):
+        t = Tensors([700], bits=bits, seed=i)
+        for step in (5, 6):
+            t.new_grads()
+            t.step(step, **kw)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("scale", [1e-18, 1e10])
+def test_gradients_far_from_one(bits, scale):
+    t = Tensors([700], bits=bits)
+    for step in (1, 2, 3):
+        t.new_grads(scale)
+        t.step(step, eps=0.0 if scale > 1 else 1e-20)
+
+
+def test_gradients_of_zero_keep_zero_moments():
+    for bits in (32, 8):
+        t = Tensors([600], bits=bits)
+        t.step(1)
+        assert not any(x.any() for x in (t.m[0], t.v[0]))
+
+
+def test_8_bit_blocks_that_are_not_finite():
+    t = Tensors([1000], bits=8)
+    t.new_grads()
+    t.grads[0][300], t.grads[0][600] = float("nan"), float("inf")
+    B.adamw_step(t.p, t.grads, t.m, t.v, 1e-3, 0.9, 0.99, 1e-8, 0.0, 1, t.ms, t.vs)
+    out = [torch.empty(1000, device="cuda") for _ in range(2)]
+    B.adamw_unpack(t.m, t.v, t.ms, t.vs, [out[0]], [out[1]])
+    for x in out:
+        assert torch.isfinite(x[:256]).all() and torch.isnan(x[256:768]).all() and torch.isfinite(x[768:]).all()
+    bad = ~torch.isfinite(t.p[0])
+    assert bad[300] and bad[600] and int(bad.sum()) == 2
+
+
+def test_unpack():
+    t = Tensors([1, 255, 257, 0, 9000], bits=8, shift=1)
+    for i, n in enumerate(t.sizes):
+        t.m[i].copy_(torch.from_numpy(t.g.integers(-127, 128, n).astype(np.int8)).cuda())
+        t.v[i].copy_(torch.from_numpy(t.g.integers(0, 256, n).astype(np.uint8)).cuda())
+        t.ms[i].copy_(torch.from_numpy(t.g.random(len(t.ms[i])).astype(np.float32)).cuda())
+        t.vs[i].copy_(torch.from_numpy(np.exp(-40 * t.g.random(len(t.vs[i]))).astype(np.float32)).cuda())
+    out = [[torch.empty(n, device="cuda") for n in t.sizes] for _ in range(2)]
+    B.adamw_unpack(t.m, t.v, t.ms, t.vs, *out)
+    for i in range(len(t.sizes)):
+        for y, ref in zip(out, t.moments(i)):
+            assert (np.abs(host(y[i]) - ref) <= U * np.abs(ref) * (1 + 1e-6) + 1e-45).all()
+
+
+def test_equal_calls_give_equal_bits():
+    a, b = (Tensors(SIZES, "bf16", "f32", 8, seed=3) for _ in range(2))
+    for step in (1, 2):
+        for t in (a, b):
+            t.new_grads()
+            B.adamw_step(t.p, t.grads, t.m, t.v, **HYPER, step=step, m_scale=t.ms, v_scale=t.vs)
+    for x, y in zip(a.p + a.m + a.v + a.ms + a.vs, b.p + b.m + b.v + b.ms + b.vs):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_recorded_steps_follow_the_scalars(bits):
+    """one recorded step replayed with the schedule in device memory, on new gradients, against eager steps"""
+    t, e = (Tensors([5000, 300, 64], bits=bits, copies=True, seed=4) for _ in range(2))
+    plan = B.PreparedAdamW(t.p, t.grads, t.m, t.v, t.ms, t.vs, t.copies)
+    eager = B.PreparedAdamW(e.p, e.grads, e.m, e.v, e.ms, e.vs, e.copies)
+    scalars = torch.zeros(4, dtype=torch.float64, device="cuda")
+    args = (HYPER["beta1"], HYPER["beta2"], HYPER["eps"], HYPER["weight_decay"])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan(0.0, *args, 1, scalars=scalars)
+    for step in range(1, 5):
+        lr = 1e-3 * step
+        for x in (t, e):
+            x.new_grads()
+        scalars.copy_(torch.tensor([lr, 1 / (1 - HYPER["beta1"] ** step), 1 / (1 - HYPER["beta2"] ** step), 0.5], dtype=torch.float64))
+        graph.replay()
+        eager(lr, *args, step, grad_scale=0.5)
+        torch.cuda.synchronize()
+        for x, y in zip(t.p + t.m + t.v + t.copies, e.p + e.m + e.v + e.copies):
+            assert torch.equal(x, y), step
+
+
+def test_on_another_stream():
+    t = Tensors([5000, 3])
+    t.new_grads()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    t.step(1, stream=side)
+
+
+# ------------------------------------------------------------------------------------------------- with what gives gradients
+def test_training_steps_of_the_recurrent_network():
+    """forward pass, backward pass by Jacobi iteration, parameter gradients and AdamW, step after step; every step against the
+    oracles from the weights it started with.  eps is of the gradients' size: the step's slope in a gradient is below lr c1 (1 - beta1) /
+    eps, so a gradient's error (1e-4 of its largest entry, as in the recurrent network's own tests) moves a weight by that much."""
+    w = S.rnn_workload("rnn_small")
+    W, U_, b = S.make_rnn_params(w)
+    params = [torch.from_numpy(a.copy()).cuda() for a in (W, U_, b)]
+    grads = [torch.empty_like(p) for p in params]
+    m, v, _, _ = B.adamw_moments(params)
+    plan = B.PreparedAdamW(params, grads, m, v)
+    z, h, d = (torch.empty(w.B, w.T, w.H, device="cuda") for _ in range(3))
+    lr, b1, b2, eps, wd = 0.01, 0.9, 0.99, 1.0, 0.01
+    for step in range(1, 4):
+        x, y = S.make_rnn_inputs(w, step)
+        xd, yd = torch.from_numpy(x).cuda(), torch.from_numpy(y).cuda()
+        before = [(host(p), host(mm), host(vv)) for p, mm, vv in zip(params, m, v)]
+        p64 = [p.double().cpu().numpy() for p in params]
+        B.rnn_forward(*params, xd, None, w.B, w.T, w.H, x.shape[2], z, h)
+        g = h - yd
+        B.rnn_backward_jacobi(params[0], z, g, None, w.B, w.T, w.H, 0, 0.0, d)
+        B.rnn_param_grads(z, h, xd, d, None, w.B, w.T, w.H, x.shape[2], *grads)
+        plan(lr, b1, b2, eps, wd, step)
+        z64, h64 = R.rnn_forward(*p64, x)
+        d64 = R.backprop_sequential(p64[0], z64, h64 - y)
+        s = 1 / (1 + np.exp(-z64)) * d64
+        prev = np.concatenate([np.zeros_like(h64[:, :1]), h64[:, :-1]], 1)
+        ref = [np.einsum("bti,btj->ij", s, prev), np.einsum("bti,btj->ij", s, x.astype(np.float64)), s.sum((0, 1))]
+        for i in range(3):
+            gr = ref[i].reshape(-1)
+            g_tol = 1e-4 * np.abs(gr).max()
+            assert np.abs(host(grads[i]) - gr).max() <= g_tol, (step, i)
+            p0, m0, v0 = before[i]
+            want, m64, v64 = A.step(p0, gr, m0, v0, lr, b1, b2, eps, wd, step)
+            # |du/dg| <= lr c1 ((1 - beta1) / eps + |m| sqrt(c2 (1 - beta2)) / eps^2)
+            c1, c2 = 1 / (1 - b1 ** step), 1 / (1 - b2 ** step)
+            slope = lr * c1 * ((1 - b1) / eps + np.abs(m64) * np.sqrt(c2 * (1 - b2)) / eps ** 2)
+            tol = 2 * slope * g_tol + U * (4 * np.abs(p0) + 32 * lr * c1 * (np.abs(m64) + np.abs(m0) + np.abs(gr)) / eps)
+            assert (np.abs(host(params[i]) - want) <= tol).all(), (step, i)
+
+
+def test_training_step_of_a_linear_attention_layer():
+    """projections of one input to q, k and v, linear attention, a quadratic loss; its gradients through linattn_backward and the
+    projections, then a step with bf16 copies for the next forward pass"""
+    g = np.random.default_rng(8)
+    Bn, T, H, Dk, Dv, I = 2, 90, 2, 16, 32, 24
+    dims = [H * Dk, H * Dk, H * Dv]
+    x = torch.from_numpy(g.normal(size=(Bn, T, I)).astype(np.float32)).cuda()
+    y = torch.from_numpy(g.normal(size=(Bn, T, H, Dv)).astype(np.float32)).cuda()
+    ld = np.array([-0.1, -0.02], np.float32)
+    Ws = [torch.from_numpy((g.normal(size=(I, n)) / I ** 0.5).astype(np.float32)).cuda() for n in dims]
+    copies = [torch.empty_like(W, dtype=torch.bfloat16) for W in Ws]
+    m, v, _, _ = B.adamw_moments(Ws)
+    q, k, vv = (torch.matmul(x, W).view(Bn, T, H, -1) for W in Ws)
+    o, grads = torch.empty(Bn, T, H, Dv, device="cuda"), [torch.empty_like(t) for t in (q, k, vv)]
+    sizes = (Bn, T, H, H, Dk, Dv, 0.25)
+    B.linattn_forward(q, k, vv, torch.from_numpy(ld).cuda(), None, None, *sizes, o)
+    B.linattn_backward(q, k, vv, torch.from_numpy(ld).cuda(), None, None, o - y, None, *sizes, *grads)
+    dW = [torch.matmul(x.reshape(-1, I).t().contiguous(), t.reshape(Bn * T, -1)) for t in grads]
+    before = [host(W) for W in Ws]
+    lr, b1, b2, eps, wd = 0.01, 0.9, 0.99, 1.0, 0.0
+    B.adamw_step(Ws, dW, m, v, lr, b1, b2, eps, wd, 1, copies=copies)
+    # the same in 64 bits, from the fp32 projections
+    refs = [np.zeros((I, n)) for n in dims]
+    for bi in range(Bn):
+        a = [t[bi].double().cpu().numpy() for t in (q, k, vv)]
+        out = L.forward(*a, ld, 0.25)[0]
+        d = L.backward(*a, ld, 0.25, out - y[bi].double().cpu().numpy())[:3]
+        for i in range(3):
+            refs[i] += x[bi].double().cpu().numpy().T @ d[i].reshape(T, -1)
+    for i in range(3):
+        gr = refs[i].reshape(-1)
+        g_tol = 2e-5 * np.abs(gr).max()          # (a hundred fp32 sums of the terms' size, in the oracle's own units)
+        assert np.abs(host(dW[i]) - gr).max() <= g_tol, i
+        want, m64, v64 = A.step(before[i], gr, 0 * gr, 0 * gr, lr, b1, b2, eps, wd, 1)
+        tol = 2 * lr / eps * g_tol + U * (4 * np.abs(before[i]) + 32 * lr * np.abs(gr) / eps)
+        assert (np.abs(host(Ws[i]) - want) <= tol).all(), i
+        assert (np.abs(host(copies[i]) - want) <= tol + 2.0 ** -8 * np.abs(want)).all(), i
