@@ -52,9 +52,10 @@ __device__ __forceinline__ int aw_find(const AdamwArgs& a, unsigned id) {
   return lo;
 }
 
-// ---- four elements from `i` on, those below n; `whole`: the quad is aligned and complete
-__device__ __forceinline__ void aw_load(const float* p, long long i, long long n, bool whole, float (&x)[4]) {
-  if (whole) {
+// ---- four elements from `i` on of a chunk with `n` elements; WHOLE: the chunk is complete and its quads are aligned
+template <bool WHOLE>
+__device__ __forceinline__ void aw_load(const float* p, unsigned i, unsigned n, float (&x)[4]) {
+  if (WHOLE) {
     const float4 f = *(const float4*)(p + i);
     x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
   } else {
@@ -62,8 +63,9 @@ __device__ __forceinline__ void aw_load(const float* p, long long i, long long n
     for (int e = 0; e < 4; ++e) x[e] = i + e < n ? p[i + e] : 0.0f;
   }
 }
-__device__ __forceinline__ void aw_load(const aw_bf16* p, long long i, long long n, bool whole, float (&x)[4]) {
-  if (whole) {
+template <bool WHOLE>
+__device__ __forceinline__ void aw_load(const aw_bf16* p, unsigned i, unsigned n, float (&x)[4]) {
+  if (WHOLE) {
     const uint2 f = *(const uint2*)(p + i);
     x[0] = __uint_as_float(f.x << 16); x[1] = __uint_as_float(f.x & 0xffff0000u);
     x[2] = __uint_as_float(f.y << 16); x[3] = __uint_as_float(f.y & 0xffff0000u);
@@ -72,15 +74,17 @@ __device__ __forceinline__ void aw_load(const aw_bf16* p, long long i, long long
     for (int e = 0; e < 4; ++e) x[e] = i + e < n ? __uint_as_float((uint32_t)p[i + e] << 16) : 0.0f;
   }
 }
-__device__ __forceinline__ uint32_t aw_load(const uint8_t* p, long long i, long long n, bool whole) {
-  if (whole) return *(const uint32_t*)(p + i);
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t aw_load(const uint8_t* p, unsigned i, unsigned n) {
+  if (WHOLE) return *(const uint32_t*)(p + i);
   uint32_t x = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) x |= i + e < n ? (uint32_t)p[i + e] << 8 * e : 0u;
   return x;
 }
-__device__ __forceinline__ void aw_store(float* p, long long i, long long n, bool whole, const float (&x)[4]) {
-  if (whole) {
+template <bool WHOLE>
+__device__ __forceinline__ void aw_store(float* p, unsigned i, unsigned n, const float (&x)[4]) {
+  if (WHOLE) {
     *(float4*)(p + i) = make_float4(x[0], x[1], x[2], x[3]);
   } else {
 #pragma unroll
@@ -88,11 +92,12 @@ __device__ __forceinline__ void aw_store(float* p, long long i, long long n, boo
       if (i + e < n) p[i + e] = x[e];
   }
 }
-__device__ __forceinline__ void aw_store(aw_bf16* p, long long i, long long n, bool whole, const float (&x)[4]) {
+template <bool WHOLE>
+__device__ __forceinline__ void aw_store(aw_bf16* p, unsigned i, unsigned n, const float (&x)[4]) {
   typedef __attribute__((ext_vector_type(4))) __bf16 quad;
   const quad h = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
   const uint2 w = __builtin_bit_cast(uint2, h);
-  if (whole) {
+  if (WHOLE) {
     *(uint2*)(p + i) = w;
   } else {
 #pragma unroll
@@ -100,8 +105,9 @@ __device__ __forceinline__ void aw_store(aw_bf16* p, long long i, long long n, b
       if (i + e < n) p[i + e] = (aw_bf16)((e < 2 ? w.x : w.y) >> 16 * (e & 1));
   }
 }
-__device__ __forceinline__ void aw_store(uint8_t* p, long long i, long long n, bool whole, uint32_t x) {
-  if (whole) {
+template <bool WHOLE>
+__device__ __forceinline__ void aw_store(uint8_t* p, unsigned i, unsigned n, uint32_t x) {
+  if (WHOLE) {
     *(uint32_t*)(p + i) = x;
   } else {
 #pragma unroll
@@ -132,26 +138,43 @@ __device__ __forceinline__ double aw_average(double b, double v, double o, doubl
 // The largest of a wave's values, none negative, by their bits: a NaN is above infinity and stays.
 __device__ __forceinline__ float aw_wave_max(float x) {
   uint32_t b = __float_as_uint(x);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) b = max(b, (uint32_t)__shfl_xor((int)b, d));
-  return __uint_as_float(b);
+  // (within rows of 16 lanes: neighbours, pairs, mirrored halves, the mirrored row; then the four rows)
+  b = max(b, (uint32_t)__builtin_amdgcn_mov_dpp((int)b, 0xB1, 0xf, 0xf, true));
+  b = max(b, (uint32_t)__builtin_amdgcn_mov_dpp((int)b, 0x4E, 0xf, 0xf, true));
+  b = max(b, (uint32_t)__builtin_amdgcn_mov_dpp((int)b, 0x141, 0xf, 0xf, true));
+  b = max(b, (uint32_t)__builtin_amdgcn_mov_dpp((int)b, 0x140, 0xf, 0xf, true));
+  const uint32_t r0 = __builtin_amdgcn_readlane((int)b, 0), r1 = __builtin_amdgcn_readlane((int)b, 16);
+  const uint32_t r2 = __builtin_amdgcn_readlane((int)b, 32), r3 = __builtin_amdgcn_readlane((int)b, 48);
+  return __uint_as_float(max(max(r0, r1), max(r2, r3)));
 }
 
-// The code of x = |moment| / scale (0 .. 1): floor(top * root(x) + 1/2).  The root is taken in fp32; where that lies within
-// 2^-9 of the border to the next code (its error is below 2^-12 steps) the border itself decides, in 64 bits.
+// 1 / x for a block's scale, off by less than 2^-40: only the first guess of a code hangs on it.
+__device__ __forceinline__ double aw_reciprocal(float x) {
+  const double d = (double)x, r = __builtin_amdgcn_rcp(d);
+  return x > 0.0f ? r * (2.0 - d * r) : 0.0;
+}
+
+// The code of a moment's share of its scale, floor(top * root(share) + 1/2), by the hardware's root (1 ulp: the product is
+// off by less than 2^-15 steps of m's codes, 2^-14 of v's).  near: the border to the next code is no further than four times that.
 template <bool SECOND>
-__device__ __forceinline__ int aw_code(double x) {
-  const float f = (float)x;
-  const float r = SECOND ? 255.0f * sqrtf(sqrtf(f)) : 127.0f * sqrtf(f);
-  const float s = r + 0.5f, c = floorf(s), d = s - c;
-  int code = (int)c;
-  if (d < 0x1p-9f || d > 1.0f - 0x1p-9f) {
-    // candidates: the code whose lower border is nearest
-    const int k = (int)floorf(s + 0x1p-8f);                      // (the border is (k - 1/2) / top)
-    const double b = (double)(2 * k - 1);
-    const double border = SECOND ? b * b * (b * b) : b * b;
-    const double y = SECOND ? x * (16.0 * AW_V) : x * (4.0 * AW_M);
-    code = k > 0 && y < border ? k - 1 : k;
+__device__ __forceinline__ int aw_guess(double share, bool& near) {
+  constexpr float margin = SECOND ? 0x1p-12f : 0x1p-13f;
+  const float f = (float)share, q = __builtin_amdgcn_sqrtf(f);
+  const float s = (SECOND ? 255.0f * __builtin_amdgcn_sqrtf(q) : 127.0f * q) + 0.5f;
+  const float c = floorf(s);
+  near |= fabsf(s - c - 0.5f) > 0.5f - margin;
+  return min((int)c, SECOND ? 255 : 127);
+}
+// The guess, put right: code k begins at scale * ((k - 1/2) / top)^2 or ^4.
+template <bool SECOND>
+__device__ __forceinline__ int aw_exact(int guess, double moment, double scale) {
+  int code = guess;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const double b = (double)(2 * (guess + k) - 1), b2 = b * b;
+    const bool reached = SECOND ? moment * (16.0 * AW_V) >= scale * (b2 * b2) : moment * (4.0 * AW_M) >= scale * b2;
+    if (k == 0 && !reached && guess > 0) code = guess - 1;
+    if (k == 1 && reached) code = guess + 1;
   }
   return min(code, SECOND ? 255 : 127);
 }
@@ -186,31 +209,29 @@ __device__ __forceinline__ float aw_new(float p, float m, float v, const AdamwNu
   return p * k.keep - k.lr_c1 * m / (sqrtf(v * k.c2) + k.eps);
 }
 
-template <typename P, typename G>
-__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(AdamwArgs a) {
-  const int which = aw_find(a, blockIdx.x);
-  const AdamwTensor& t = a.t[which];
-  const long long n = t.n, base = (long long)(blockIdx.x - a.first[which]) * AW_CHUNK;
-  P* p = (P*)t.p;
-  const G* g = (const G*)t.g;
-  float *m = (float*)t.m, *v = (float*)t.v;
-  aw_bf16* copy = (aw_bf16*)t.copy;
-  const AdamwNumbers k = aw_numbers(a);
+// The update where v may lie below the normal numbers: the hardware's root (1 ulp) of a value that it takes, and its reciprocal (1 ulp).
+__device__ __forceinline__ float aw_new_fast(float p, float m, float v, const AdamwNumbers& k) {
+  const float x = v * k.c2;
+  const bool tiny = x < 0x1p-96f;
+  const float root = __builtin_amdgcn_sqrtf(tiny ? x * 0x1p64f : x) * (tiny ? 0x1p-32f : 1.0f);
+  return p * k.keep - k.lr_c1 * m * __builtin_amdgcn_rcpf(root + k.eps);
+}
+
+template <bool WHOLE, typename P, typename G>
+__device__ __forceinline__ void aw_chunk(P* p, const G* g, float* m, float* v, aw_bf16* copy, unsigned n, const AdamwNumbers& k) {
   const float b1 = (float)k.b1, b2 = (float)k.b2, o1 = (float)k.one_b1, o2 = (float)k.one_b2, gs = (float)k.gs;
-  const bool whole = (((uintptr_t)m | (uintptr_t)v) & 15) == 0 && ((uintptr_t)p & (4 * sizeof(P) - 1)) == 0 &&
-                     ((uintptr_t)g & (4 * sizeof(G) - 1)) == 0 && ((uintptr_t)copy & 7) == 0 && base + AW_CHUNK <= n;
   float pv[AW_ITEMS][4], gv[AW_ITEMS][4], mv[AW_ITEMS][4], vv[AW_ITEMS][4];
 #pragma unroll
   for (int i = 0; i < AW_ITEMS; ++i) {
-    const long long at = base + (long long)(i * AW_THREADS + threadIdx.x) * 4;
-    aw_load(p, at, n, whole, pv[i]);
-    aw_load(g, at, n, whole, gv[i]);
-    aw_load(m, at, n, whole, mv[i]);
-    aw_load(v, at, n, whole, vv[i]);
+    const unsigned at = (i * AW_THREADS + threadIdx.x) * 4;
+    aw_load<WHOLE>(p, at, n, pv[i]);
+    aw_load<WHOLE>(g, at, n, gv[i]);
+    aw_load<WHOLE>(m, at, n, mv[i]);
+    aw_load<WHOLE>(v, at, n, vv[i]);
   }
 #pragma unroll
   for (int i = 0; i < AW_ITEMS; ++i) {
-    const long long at = base + (long long)(i * AW_THREADS + threadIdx.x) * 4;
+    const unsigned at = (i * AW_THREADS + threadIdx.x) * 4;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float x = gv[i][e] * gs;
@@ -218,46 +239,66 @@ __global__ __launch_bounds__(AW_THREADS) void adamw_kernel(AdamwArgs a) {
       vv[i][e] = b2 * vv[i][e] + o2 * (x * x);
       pv[i][e] = aw_new(pv[i][e], mv[i][e], vv[i][e], k);
     }
-    aw_store(m, at, n, whole, mv[i]);
-    aw_store(v, at, n, whole, vv[i]);
-    aw_store(p, at, n, whole, pv[i]);
-    if (copy) aw_store(copy, at, n, whole, pv[i]);
+    aw_store<WHOLE>(m, at, n, mv[i]);
+    aw_store<WHOLE>(v, at, n, vv[i]);
+    aw_store<WHOLE>(p, at, n, pv[i]);
+    if (copy) aw_store<WHOLE>(copy, at, n, pv[i]);
   }
+}
+
+// The chunk of this workgroup: its place in the tensor and how many elements it has.
+struct AdamwChunk {
+  long long base;
+  unsigned n;
+};
+__device__ __forceinline__ const AdamwTensor& aw_chunk_of(const AdamwArgs& a, AdamwChunk& c) {
+  const int which = aw_find(a, blockIdx.x);
+  c.base = (long long)(blockIdx.x - a.first[which]) * AW_CHUNK;
+  c.n = (unsigned)min((long long)AW_CHUNK, a.t[which].n - c.base);
+  return a.t[which];
+}
+__device__ __forceinline__ bool aw_aligned(const void* p, unsigned bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+template <typename P, typename G>
+__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(AdamwArgs a) {
+  AdamwChunk c;
+  const AdamwTensor& t = aw_chunk_of(a, c);
+  P* p = (P*)t.p + c.base;
+  const G* g = (const G*)t.g + c.base;
+  float *m = (float*)t.m + c.base, *v = (float*)t.v + c.base;
+  aw_bf16* copy = t.copy ? (aw_bf16*)t.copy + c.base : nullptr;
+  const AdamwNumbers k = aw_numbers(a);
+  if (c.n == AW_CHUNK && aw_aligned(p, 4 * sizeof(P)) && aw_aligned(g, 4 * sizeof(G)) && aw_aligned(m, 16) && aw_aligned(v, 16) && aw_aligned(copy, 8))
+    aw_chunk<true>(p, g, m, v, copy, c.n, k);
+  else
+    aw_chunk<false>(p, g, m, v, copy, c.n, k);
 }
 
 // Moments in 8 bits: a wave takes whole blocks, four elements a lane, and agrees on the scale by exchange among its lanes.
 // Moments are formed in 64 bits (this device's rate for them is that of 32): a code then does not hang on how an fp32 sum
-// next to the border of two codes was rounded.
-template <typename P, typename G>
-__global__ __launch_bounds__(AW_THREADS) void adamw_8bit_kernel(AdamwArgs a) {
-  const int which = aw_find(a, blockIdx.x);
-  const AdamwTensor& t = a.t[which];
-  const long long n = t.n, base = (long long)(blockIdx.x - a.first[which]) * AW_CHUNK;
-  P* p = (P*)t.p;
-  const G* g = (const G*)t.g;
-  uint8_t *m = (uint8_t*)t.m, *v = (uint8_t*)t.v;
-  aw_bf16* copy = (aw_bf16*)t.copy;
-  const AdamwNumbers k = aw_numbers(a);
-  const bool whole = (((uintptr_t)m | (uintptr_t)v) & 3) == 0 && ((uintptr_t)p & (4 * sizeof(P) - 1)) == 0 &&
-                     ((uintptr_t)g & (4 * sizeof(G) - 1)) == 0 && ((uintptr_t)copy & 7) == 0 && base + AW_CHUNK <= n;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// next to the border of two codes was rounded.  Codes are guessed in fp32; where a lane's guess is too close to a border (one
+// quad in a thousand, one wave's in nine) the wave compares with the borders in 64 bits.
+template <bool WHOLE, typename P, typename G>
+__device__ __forceinline__ void aw_chunk_8bit(P* p, const G* g, uint8_t* m, uint8_t* v, float* m_scale, float* v_scale, aw_bf16* copy, unsigned n,
+                                              const AdamwNumbers& k) {
+  const unsigned lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float pv[AW_ITEMS][4], gv[AW_ITEMS][4], ms[AW_ITEMS], vs[AW_ITEMS];
   uint32_t mc[AW_ITEMS], vc[AW_ITEMS];
 #pragma unroll
   for (int i = 0; i < AW_ITEMS; ++i) {
-    const long long block = base / ADAMW_BLOCK + i * (AW_THREADS / 64) + wave, at = block * ADAMW_BLOCK + 4 * lane;
-    const bool there = block * ADAMW_BLOCK < n;
-    ms[i] = there ? t.ms[block] : 0.0f;
-    vs[i] = there ? t.vs[block] : 0.0f;
-    mc[i] = aw_load(m, at, n, whole);
-    vc[i] = aw_load(v, at, n, whole);
-    aw_load(p, at, n, whole, pv[i]);
-    aw_load(g, at, n, whole, gv[i]);
+    const unsigned block = i * (AW_THREADS / 64) + wave, at = block * ADAMW_BLOCK + 4 * lane;
+    const bool there = WHOLE || block * ADAMW_BLOCK < n;
+    ms[i] = there ? m_scale[block] : 0.0f;
+    vs[i] = there ? v_scale[block] : 0.0f;
+    mc[i] = aw_load<WHOLE>(m, at, n);
+    vc[i] = aw_load<WHOLE>(v, at, n);
+    aw_load<WHOLE>(p, at, n, pv[i]);
+    aw_load<WHOLE>(g, at, n, gv[i]);
   }
 #pragma unroll
   for (int i = 0; i < AW_ITEMS; ++i) {
-    const long long block = base / ADAMW_BLOCK + i * (AW_THREADS / 64) + wave, at = block * ADAMW_BLOCK + 4 * lane;
-    if (block * ADAMW_BLOCK >= n) break;                             // (the wave's: elements behind n are zeros below)
+    const unsigned block = i * (AW_THREADS / 64) + wave, at = block * ADAMW_BLOCK + 4 * lane;
+    if (!WHOLE && block * ADAMW_BLOCK >= n) break;                   // (the wave's: elements behind n are zeros below)
     double md[4], vd[4];
     float mm = 0.0f, vm = 0.0f;
 #pragma unroll
@@ -265,65 +306,98 @@ __global__ __launch_bounds__(AW_THREADS) void adamw_8bit_kernel(AdamwArgs a) {
       const double x = (double)gv[i][e] * k.gs;
       md[e] = aw_average(k.b1, aw_value_m((int)(int8_t)(mc[i] >> 8 * e), ms[i]), k.one_b1, x);
       vd[e] = aw_average(k.b2, aw_value_v((int)(vc[i] >> 8 * e & 255), vs[i]), k.one_b2 * x, x);
-      if (at + e >= n) md[e] = vd[e] = 0.0;
+      if (!WHOLE && at + e >= n) md[e] = vd[e] = 0.0;
       const float mf = (float)md[e], vf = (float)vd[e];
-      pv[i][e] = aw_new(pv[i][e], mf, vf, k);
+      pv[i][e] = aw_new_fast(pv[i][e], mf, vf, k);
       mm = __uint_as_float(max(__float_as_uint(mm), __float_as_uint(fabsf(mf))));
       vm = __uint_as_float(max(__float_as_uint(vm), __float_as_uint(vf)));
     }
+    aw_store<WHOLE>(p, at, n, pv[i]);
+    if (copy) aw_store<WHOLE>(copy, at, n, pv[i]);
     mm = aw_wave_max(mm);
     vm = aw_wave_max(vm);
-    const double mi = mm > 0.0f ? 1.0 / (double)mm : 0.0, vi = vm > 0.0f ? 1.0 / (double)vm : 0.0;
+    const double mi = aw_reciprocal(mm), vi = aw_reciprocal(vm);
+    int c[4], d[4];
+    bool near = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      c[e] = aw_guess<false>(fabs(md[e]) * mi, near);
+      d[e] = aw_guess<true>(vd[e] * vi, near);
+    }
+    if (__any(near)) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (mm > 0.0f) c[e] = aw_exact<false>(c[e], fabs(md[e]), mm);
+        if (vm > 0.0f) d[e] = aw_exact<true>(d[e], vd[e], vm);
+      }
+    }
     uint32_t mo = 0, vo = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int c = aw_code<false>(fabs(md[e]) * mi);
-      int d = aw_code<true>(vd[e] * vi);
-      d = vd[e] > 0.0 ? max(d, 1) : d;
-      mo |= ((uint32_t)(md[e] < 0.0 ? -c : c) & 255u) << 8 * e;
-      vo |= ((uint32_t)d & 255u) << 8 * e;
+      mo |= ((uint32_t)(md[e] < 0.0 ? -c[e] : c[e]) & 255u) << 8 * e;
+      vo |= ((uint32_t)(vd[e] > 0.0 ? max(d[e], 1) : d[e]) & 255u) << 8 * e;
     }
-    aw_store(m, at, n, whole, mo);
-    aw_store(v, at, n, whole, vo);
-    aw_store(p, at, n, whole, pv[i]);
-    if (copy) aw_store(copy, at, n, whole, pv[i]);
+    aw_store<WHOLE>(m, at, n, mo);
+    aw_store<WHOLE>(v, at, n, vo);
     if (lane == 0) {
-      t.ms[block] = mm + (mm - mm);          // (NaN also where the largest is infinite)
-      t.vs[block] = vm + (vm - vm);
+      m_scale[block] = mm + (mm - mm);          // (NaN also where the largest is infinite)
+      v_scale[block] = vm + (vm - vm);
     }
   }
 }
 
-// Values of 8-bit moments: p is the output of m, copy that of v.
-__global__ __launch_bounds__(AW_THREADS) void adamw_unpack_kernel(AdamwArgs a) {
-  const int which = aw_find(a, blockIdx.x);
-  const AdamwTensor& t = a.t[which];
-  const long long n = t.n, base = (long long)(blockIdx.x - a.first[which]) * AW_CHUNK;
-  const uint8_t *m = (const uint8_t*)t.m, *v = (const uint8_t*)t.v;
-  float *mo = (float*)t.p, *vo = (float*)t.copy;
-  const bool whole = (((uintptr_t)m | (uintptr_t)v) & 3) == 0 && (((uintptr_t)mo | (uintptr_t)vo) & 15) == 0 && base + AW_CHUNK <= n;
+template <typename P, typename G>
+__global__ __launch_bounds__(AW_THREADS) void adamw_8bit_kernel(AdamwArgs a) {
+  AdamwChunk c;
+  const AdamwTensor& t = aw_chunk_of(a, c);
+  P* p = (P*)t.p + c.base;
+  const G* g = (const G*)t.g + c.base;
+  uint8_t *m = (uint8_t*)t.m + c.base, *v = (uint8_t*)t.v + c.base;
+  aw_bf16* copy = t.copy ? (aw_bf16*)t.copy + c.base : nullptr;
+  float *ms = t.ms + c.base / ADAMW_BLOCK, *vs = t.vs + c.base / ADAMW_BLOCK;
+  const AdamwNumbers k = aw_numbers(a);
+  if (c.n == AW_CHUNK && aw_aligned(p, 4 * sizeof(P)) && aw_aligned(g, 4 * sizeof(G)) && aw_aligned(m, 4) && aw_aligned(v, 4) && aw_aligned(copy, 8))
+    aw_chunk_8bit<true>(p, g, m, v, ms, vs, copy, c.n, k);
+  else
+    aw_chunk_8bit<false>(p, g, m, v, ms, vs, copy, c.n, k);
+}
+
+template <bool WHOLE>
+__device__ __forceinline__ void aw_chunk_unpack(const uint8_t* m, const uint8_t* v, const float* m_scale, const float* v_scale, float* mo, float* vo,
+                                                unsigned n) {
   uint32_t mc[AW_ITEMS], vc[AW_ITEMS];
   float ms[AW_ITEMS], vs[AW_ITEMS];
 #pragma unroll
   for (int i = 0; i < AW_ITEMS; ++i) {
-    const long long at = base + (long long)(i * AW_THREADS + threadIdx.x) * 4;
-    ms[i] = at < n ? t.ms[at / ADAMW_BLOCK] : 0.0f;
-    vs[i] = at < n ? t.vs[at / ADAMW_BLOCK] : 0.0f;
-    mc[i] = aw_load(m, at, n, whole);
-    vc[i] = aw_load(v, at, n, whole);
+    const unsigned at = (i * AW_THREADS + threadIdx.x) * 4;
+    ms[i] = at < n ? m_scale[at / ADAMW_BLOCK] : 0.0f;
+    vs[i] = at < n ? v_scale[at / ADAMW_BLOCK] : 0.0f;
+    mc[i] = aw_load<WHOLE>(m, at, n);
+    vc[i] = aw_load<WHOLE>(v, at, n);
   }
 #pragma unroll
   for (int i = 0; i < AW_ITEMS; ++i) {
-    const long long at = base + (long long)(i * AW_THREADS + threadIdx.x) * 4;
+    const unsigned at = (i * AW_THREADS + threadIdx.x) * 4;
     float x[4], y[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       x[e] = (float)aw_value_m((int)(int8_t)(mc[i] >> 8 * e), ms[i]);
       y[e] = (float)aw_value_v((int)(vc[i] >> 8 * e & 255), vs[i]);
     }
-    aw_store(mo, at, n, whole, x);
-    aw_store(vo, at, n, whole, y);
+    aw_store<WHOLE>(mo, at, n, x);
+    aw_store<WHOLE>(vo, at, n, y);
   }
+}
+
+// Values of 8-bit moments: p is the output of m, copy that of v.
+__global__ __launch_bounds__(AW_THREADS) void adamw_unpack_kernel(AdamwArgs a) {
+  AdamwChunk c;
+  const AdamwTensor& t = aw_chunk_of(a, c);
+  const uint8_t *m = (const uint8_t*)t.m + c.base, *v = (const uint8_t*)t.v + c.base;
+  const float *ms = t.ms + c.base / ADAMW_BLOCK, *vs = t.vs + c.base / ADAMW_BLOCK;
+  float *mo = (float*)t.p + c.base, *vo = (float*)t.copy + c.base;
+  if (c.n == AW_CHUNK && aw_aligned(m, 4) && aw_aligned(v, 4) && aw_aligned(mo, 16) && aw_aligned(vo, 16)) aw_chunk_unpack<true>(m, v, ms, vs, mo, vo, c.n);
+  else aw_chunk_unpack<false>(m, v, ms, vs, mo, vo, c.n);
 }
 
 }  // namespace jm
