@@ -163,7 +163,7 @@ __device__ __forceinline__ int aw_guess(double share, bool& near) {
   const float s = (SECOND ? 255.0f * __builtin_amdgcn_sqrtf(q) : 127.0f * q) + 0.5f;
   const float c = floorf(s);
   near |= fabsf(s - c - 0.5f) > 0.5f - margin;
-  return min((int)c, SECOND ? 255 : 127);
+  return (int)c;                       // (a share is at most 1 + 2^-23: never above the last code)
 }
 // The guess, put right: code k begins at scale * ((k - 1/2) / top)^2 or ^4.
 template <bool SECOND>

@@ -97,31 +97,18 @@ bool pieces(const LinattnView& v, int dtype) {
   return !v.p || ((uintptr_t)v.p % 16 == 0 && v.ld * size % 16 == 0 && v.dim * size % 16 == 0);
 }
 
-template <typename T, int KT, int VT, bool OUT, bool VEC>
-void launch_walk(const LinattnArgs& a, hipStream_t s) {
+template <bool OUT, bool VEC>
+void launch_walk(int dtype, int n, const LinattnArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(((long long)a.slots * a.kv_heads + 7) / 8 * 8 * a.roles));
-  if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((linattn_walk_bf16_kernel<KT, VT, OUT, VEC>), grid, dim3(128 * VT), 0, s, a);
-  else hipLaunchKernelGGL((linattn_walk_f32_kernel<KT, VT, OUT, VEC>), grid, dim3(64 * VT), 0, s, a);
-}
-
-template <typename T, bool OUT>
-void launch_walk(const LinattnArgs& a, bool vec, hipStream_t s) {
-  const int kt = tiles(a.role[0].dk), vt = tiles(a.role[0].dv);
-  // (operands that are fetched element by element: the square shapes do for all)
-  switch (vec ? 10 * kt + vt : std::max(kt, vt)) {
-    case 11: return launch_walk<T, 1, 1, OUT, true>(a, s);
-    case 12: return launch_walk<T, 1, 2, OUT, true>(a, s);
-    case 14: return launch_walk<T, 1, 4, OUT, true>(a, s);
-    case 21: return launch_walk<T, 2, 1, OUT, true>(a, s);
-    case 22: return launch_walk<T, 2, 2, OUT, true>(a, s);
-    case 24: return launch_walk<T, 2, 4, OUT, true>(a, s);
-    case 41: return launch_walk<T, 4, 1, OUT, true>(a, s);
-    case 42: return launch_walk<T, 4, 2, OUT, true>(a, s);
-    case 44: return launch_walk<T, 4, 4, OUT, true>(a, s);
-    case 1: return launch_walk<T, 1, 1, OUT, false>(a, s);
-    case 2: return launch_walk<T, 2, 2, OUT, false>(a, s);
-    default: return launch_walk<T, 4, 4, OUT, false>(a, s);
+#define JM_WALK(N)                                                                                              \
+  if (dtype == MADE_BF16) hipLaunchKernelGGL((linattn_walk_bf16_kernel<N, OUT, VEC>), grid, dim3(128 * N), 0, s, a); \
+  else hipLaunchKernelGGL((linattn_walk_f32_kernel<N, OUT, VEC>), grid, dim3(64 * N), 0, s, a)
+  switch (n) {
+    case 1: JM_WALK(1); break;
+    case 2: JM_WALK(2); break;
+    default: JM_WALK(4); break;
   }
+#undef JM_WALK
 }
 
 void launch_walk(int dtype, const LinattnArgs& a, bool out, hipStream_t s) {
@@ -130,8 +117,9 @@ void launch_walk(int dtype, const LinattnArgs& a, bool out, hipStream_t s) {
     const LinattnRole& r = a.role[i];
     vec = vec && pieces(r.k, dtype) && pieces(r.v, dtype) && (!out || (pieces(r.q, dtype) && pieces(r.o, dtype)));
   }
-  if (dtype == MADE_BF16) out ? launch_walk<la_bf16, true>(a, vec, s) : launch_walk<la_bf16, false>(a, vec, s);
-  else out ? launch_walk<float, true>(a, vec, s) : launch_walk<float, false>(a, vec, s);
+  const int n = tiles(std::max(a.role[0].dk, a.role[0].dv));      // (the roles of a call have the same two widths)
+  if (out) vec ? launch_walk<true, true>(dtype, n, a, s) : launch_walk<true, false>(dtype, n, a, s);
+  else vec ? launch_walk<false, true>(dtype, n, a, s) : launch_walk<false, false>(dtype, n, a, s);
 }
 
 void launch_join(const LinattnArgs& a, hipStream_t s) {
@@ -291,16 +279,8 @@ extern "C" int linattn_backward(const linattn_config* cfg, const void* q, const 
   a.role[0] = Q;
   a.role[1] = K;
   a.role[2] = R;
-  if (tiles(c.Dk) == tiles(c.Dv)) {
-    a.roles = 3;
-    launch_walk(c.dtype, a, true, s);
-  } else {
-    a.roles = 2;
-    launch_walk(c.dtype, a, true, s);
-    a.roles = 1;
-    a.role[0] = R;
-    launch_walk(c.dtype, a, true, s);
-  }
+  a.roles = 3;
+  launch_walk(c.dtype, a, true, s);
   HIP_TRY(hipGetLastError());
   return MADE_OK;
 }

@@ -276,14 +276,14 @@ __device__ __forceinline__ la_u32x4 la_rest(la_f32x8 x, la_u32x4 hi) { return la
 // that order: q and k by rows (dims), k and v by columns (steps).
 constexpr int LA_FADE = 32;     // place of the factor lambda^0 in the table
 
-template <int KT, int VT, bool OUT>
+template <int KT, bool OUT>
 struct LaLds {
   // 16-byte units of a row and of a column are exchanged (la_row_swizzle, la_swizzle) so that the 16 rows or columns an
   // operand is read from lie in different banks
   __align__(16) unsigned char q[OUT ? 64 * KT * 64 : 16];
   __align__(16) unsigned char k[OUT ? 64 * KT * 64 : 16];
   __align__(16) unsigned char kt[KT * 32 * 128];
-  __align__(16) unsigned char vt[VT * 32 * 128];
+  __align__(16) unsigned char vt[KT * 32 * 128];
   __align__(16) unsigned char p[OUT ? 6 : 1][2][64 * 16];        // scores as operands: pair of tiles, part, lane
   __align__(16) float fade[OUT ? LA_FADE + 64 : 4];              // p_scale lambda^m at LA_FADE + m, zeros before
   __align__(16) float weight[64];                                // lambda^(n-1+late-j): what the block's end keeps of step j
@@ -356,10 +356,12 @@ __device__ __forceinline__ la_f32x4 la_mfma16(la_u32x4 x, la_u32x4 y, la_f32x4 c
 
 // OUT = true: the walk with outputs.  OUT = false: only the state a segment adds, from zero, into the workspace.
 // VEC: every operand's rows come in 16-byte pieces (else none is taken to).
-template <int KT, int VT, bool OUT, bool VEC>
-__global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_kernel(LinattnArgs a) {
-  constexpr int C = LA_BF16_ROWS, NT = 128 * VT, NW = 2 * VT;
-  __shared__ LaLds<KT, VT, OUT> lds;
+// The second half of the keys, and waves of values, that a role does not have are passed over, so that one kernel of N x 32 keys and values
+// serves the roles of a gradient together.
+template <int N, bool OUT, bool VEC>
+__global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_kernel(LinattnArgs a) {
+  constexpr int C = LA_BF16_ROWS, KT = N, VT = N, NT = 128 * VT, NW = 2 * VT;
+  __shared__ LaLds<N, OUT> lds;
   LinattnPlace w;
   if (!la_place(a, OUT, w)) return;
   const LinattnRole& R = a.role[w.which];
@@ -393,6 +395,7 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
     for (int i = threadIdx.x; i < LA_FADE + 64; i += NT) lds.fade[i] = i < LA_FADE ? 0.0f : R.p_scale * la_pow(g2, i - LA_FADE);
   }
 
+  const bool mine = 16 * wave < dv;            // this wave has values
   const int stages = gq > gk ? gq : gk;
   const auto q_head = [&](int st) { return head * gq + (gq > 1 ? st : 0); };
   const auto k_head = [&](int st) { return head * gk + (gk > 1 ? st : 0); };
@@ -523,7 +526,7 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
           *(la_u32x4*)&lds.p[pair][0][lane * 16] = hi;
           *(la_u32x4*)&lds.p[pair][1][lane * 16] = la_rest(x, hi);
         }
-        if (new_q) {
+        if (new_q && mine) {
           const int lane = la_lane_id();
           // (la_row_swizzle(16 it + c) = la_row_swizzle(c))
           const unsigned char* q_ = lds.q + (lane & 15) * (KT * 64);
@@ -535,6 +538,7 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
           for (int it = 0; it < 4; ++it) qf[0][it] = q_frag(it, 0);
 #pragma unroll
           for (int kb = 0; kb < KT; ++kb) {
+            if (2 * kb == KT && 32 * kb >= dk) break;
             // (the next operands are on their way while these are multiplied; equal accumulators lie four MFMAs apart)
             if (kb + 1 < KT) {
 #pragma unroll
@@ -559,6 +563,7 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
         }
         __syncthreads();
       }
+      if (!mine) continue;
       const int lane = la_lane_id(), cl = lane & 15, g = lane >> 4;
       // (la_swizzle(16 t + c) = la_swizzle(c) ^ t for c < 16)
       const unsigned char* kt_ = lds.kt + cl * 128;
@@ -613,6 +618,7 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
           const la_u32x4 h0 = la_round(x), h1 = la_rest(x, h0);
 #pragma unroll
           for (int t = 0; t < 2 * KT; ++t) {
+            if (t == KT && 16 * t >= dk) break;
             const la_u32x4 kf = kt_frag(t, kb);
             S[t] = la_mfma16(kf, h0, S[t]);
             S[t] = la_mfma16(kf, h1, S[t]);
@@ -621,7 +627,10 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
             asm volatile("" ::: "memory");      // (k is read again, not kept)
             const la_u32x4 h2 = la_rest(x - la_widen(h0), h1);
 #pragma unroll
-            for (int t = 0; t < 2 * KT; ++t) S[t] = la_mfma16(kt_frag(t, kb), h2, S[t]);
+            for (int t = 0; t < 2 * KT; ++t) {
+              if (t == KT && 16 * t >= dk) break;
+              S[t] = la_mfma16(kt_frag(t, kb), h2, S[t]);
+            }
           }
         }
       }
@@ -647,15 +656,15 @@ __global__ __launch_bounds__(128 * VT, KT > VT ? 2 : 4) void linattn_walk_bf16_k
 
 // ---- fp32: blocks of 32 steps, 32 x 32 x 2 MFMA (an accumulator's rows are operand values as they lie, so nothing is turned
 // over).  Wave w holds the value columns 32 w .. 32 w + 31.
-template <int KT, int VT, bool OUT>
+template <int KT, bool OUT>
 struct LaLdsF32 {
-  static constexpr int PITCH = KT * 32 + 4, VPITCH = VT * 32 + 4;
+  static constexpr int PITCH = KT * 32 + 4, VPITCH = PITCH;
   __align__(16) float q[OUT ? 32 * PITCH : 4];
   __align__(16) float k[32 * PITCH];
   __align__(16) float v[32 * VPITCH];
   __align__(16) float weight[32];
   __align__(16) float fade[64];
-  la_f32x4 p[OUT ? VT : 1][4][64];     // each wave's share of the scores' sums: quad of rows, lane
+  la_f32x4 p[OUT ? KT : 1][4][64];     // each wave's share of the scores' sums: quad of rows, lane
 };
 
 template <int TILES, int NT>
@@ -681,10 +690,10 @@ __device__ __forceinline__ void la_put_rows(const la_u32x4 (&r)[PER][4], float* 
   }
 }
 
-template <int KT, int VT, bool OUT, bool VEC>
-__global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_f32_kernel(LinattnArgs a) {
-  constexpr int C = LA_F32_ROWS, NT = 64 * VT;
-  __shared__ LaLdsF32<KT, VT, OUT> lds;
+template <int N, bool OUT, bool VEC>
+__global__ __launch_bounds__(64 * N, 2) void linattn_walk_f32_kernel(LinattnArgs a) {
+  constexpr int C = LA_F32_ROWS, KT = N, VT = N, NT = 64 * VT;
+  __shared__ LaLdsF32<N, OUT> lds;
   LinattnPlace w;
   if (!la_place(a, OUT, w)) return;
   const LinattnRole& R = a.role[w.which];
@@ -720,6 +729,7 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_f32_ker
     row_in = R.i_scale * la_pow(g2, cl + 1 - late);
   }
 
+  const bool mine = 32 * wave < dv;            // this wave has values
   const int stages = gq > gk ? gq : gk;
   const auto q_head = [&](int st) { return head * gq + (gq > 1 ? st : 0); };
   const auto k_head = [&](int st) { return head * gk + (gk > 1 ? st : 0); };
@@ -782,6 +792,7 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_f32_ker
 #pragma unroll
         for (int i = 0; i < 4 * KT / VT; ++i) {
           const int m = wave + i * VT;
+          if (8 * m >= dk) break;
           const float4 k4 = *(const float4*)(k_ + 8 * m), q4 = *(const float4*)(q_ + 8 * m);
           P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.x, q4.x, P, 0, 0, 0);
           P = __builtin_amdgcn_mfma_f32_32x32x2f32(k4.y, q4.y, P, 0, 0, 0);
@@ -790,10 +801,11 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_f32_ker
         }
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj) lds.p[wave][jj][lane] = la_f32x4{P[4 * jj], P[4 * jj + 1], P[4 * jj + 2], P[4 * jj + 3]};
-        if (new_q) {
+        if (new_q && mine) {
           O = la_f32x16{};
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt)
+          for (int kt = 0; kt < KT; ++kt) {
+            if (kt > 0 && 32 * kt >= dk) break;
 #pragma unroll
             for (int jj = 0; jj < 4; ++jj) {
               const float4 q4 = *(const float4*)(q_ + 32 * kt + 8 * jj);
@@ -802,10 +814,12 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_f32_ker
               O = __builtin_amdgcn_mfma_f32_32x32x2f32(S[kt][4 * jj + 2], q4.z, O, 0, 0, 0);
               O = __builtin_amdgcn_mfma_f32_32x32x2f32(S[kt][4 * jj + 3], q4.w, O, 0, 0, 0);
             }
+          }
 #pragma unroll
           for (int e = 0; e < 16; ++e) O[e] *= row_in;
         }
         __syncthreads();
+        if (!mine) continue;
         const float* f = lds.fade + 31 + cl - 4 * hh;
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj) {
@@ -819,18 +833,22 @@ __global__ __launch_bounds__(64 * VT, KT > VT ? 1 : 2) void linattn_walk_f32_ker
         for (int e = 0; e < 16; ++e)
           O = __builtin_amdgcn_mfma_f32_32x32x2f32(v_[(8 * (e / 4) + e % 4) * lds.VPITCH], P[e], O, 0, 0, 0);
       }
+      if (!mine) continue;
       if (gk > 1 ? st == 0 : last) {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) S[kt] *= keep;
       }
       if (gk > 1 || last) {
         const float* k_ = lds.k + 4 * hh * lds.PITCH + cl;
+        la_f32x16 x;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = 8 * (e / 4) + e % 4;
-          const float x = v_[j * lds.VPITCH] * lds.weight[j + 4 * hh];
+        for (int e = 0; e < 16; ++e) x[e] = v_[(8 * (e / 4) + e % 4) * lds.VPITCH] * lds.weight[8 * (e / 4) + e % 4 + 4 * hh];
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt) S[kt] = __builtin_amdgcn_mfma_f32_32x32x2f32(k_[j * lds.PITCH + 32 * kt], x, S[kt], 0, 0, 0);
+        for (int kt = 0; kt < KT; ++kt) {
+          if (kt > 0 && 32 * kt >= dk) break;
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            S[kt] = __builtin_amdgcn_mfma_f32_32x32x2f32(k_[(8 * (e / 4) + e % 4) * lds.PITCH + 32 * kt], x[e], S[kt], 0, 0, 0);
         }
       }
 
