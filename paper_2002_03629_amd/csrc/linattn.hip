@@ -37,10 +37,11 @@ int check(const char* who, const linattn_config* c, bool step) {
   return MADE_OK;
 }
 
-// How a call's sequences are cut.  rows: of a segment; slots: segments in all.
+// How a call's sequences are cut.  rows: of a segment; slots: segments in all; q_split: workgroups that share a state's query heads.
 struct Split {
   int rows, slots;
   bool on;
+  int q_split;
 };
 
 int tiles(int d) { return d <= 32 ? 1 : d <= 64 ? 2 : 4; }
@@ -55,27 +56,33 @@ Split choose(const linattn_config& c, bool backward) {
   const int C = block_rows(c);
   const long long blocks = ((long long)c.T + C - 1) / C;     // of the longest sequence there may be
   const int whole_rows = (int)std::min<long long>(std::max<long long>(blocks, 1) * C, 0x7fffffff / C * C);
-  Split best = {whole_rows, c.B, false};
+  Split best = {whole_rows, c.B, false, 1};
   const int group = c.heads / c.kv_heads;
   const double size = (c.dtype == MADE_BF16 ? 1.0 : 1.55) * (0.55 + 0.45 * tiles(c.Dk) * tiles(c.Dv) / 16.0);
-  const double walk = size * (4.4 + 3.2 * (group - 1)), sums = size * 1.9 * (backward ? 0.5 * (1 + group) : 1.0);
-  const double heads = (double)c.kv_heads;
+  const double sums = size * 1.9 * (backward ? 0.5 * (1 + group) : 1.0), heads = (double)c.kv_heads;
   auto turns = [](double n) { return n <= UNITS ? 1.0 : 1.7 * std::ceil(n / (2 * UNITS)); };
-  double least = turns(c.B * heads * (backward ? 3 : 1)) * (walk * (double)blocks + 4.0);
-  long long last = blocks;
-  for (long long m = 2; m <= blocks && m <= 4096; ++m) {
-    const long long L = (blocks + m - 1) / m;
+  double least = 1e300;
+  // (segments about an eighth apart in number; all divisors of a group are tried, whose passes each walk the state again)
+  for (long long m = 1, last = 0; m <= std::max<long long>(blocks, 1) && m <= 1 << 20; m += std::max<long long>(1, m / 8)) {
+    const long long L = std::max<long long>(1, (blocks + m - 1) / m);
     if (L == last) continue;
     last = L;
-    const double slots = c.offsets ? (double)(blocks / L + c.B) : (double)((blocks + L - 1) / L) * c.B;
+    const bool cut = L < blocks;
+    const double slots = !cut ? c.B : c.offsets ? (double)(blocks / L + c.B) : (double)((blocks + L - 1) / L) * c.B;
     const double states = slots * heads * c.Dk * c.Dv * 4.0 * (backward ? 2 : 1);
-    const double cost = turns(slots * heads * (backward ? 3 : 1)) * (walk * (double)L + 4.0) +
-                        turns(slots * heads * (backward ? 2 : 1)) * (sums * (double)L + 2.0) + states * 3.0 / 5e6 + 8.0;
-    if (cost < least && slots < 1e9) {
-      least = cost;
-      best.rows = (int)(L * C);
-      best.slots = (int)slots;
-      best.on = true;
+    const double extra = !cut ? 0.0 : turns(slots * heads * (backward ? 2 : 1)) * (sums * (double)L + 2.0) + states * 3.0 / 5e6 + 8.0;
+    for (int q = 1; q <= (backward ? 1 : group); ++q) {
+      if (group % q != 0) continue;
+      const double walk = size * (4.4 + 3.2 * (group / q - 1));
+      const double cost = turns(slots * heads * q * (backward ? 3 : 1)) * (walk * (double)L + 4.0) + extra;
+      if (cost < least && slots < 1e9) {
+        least = cost;
+        best.rows = cut ? (int)(L * C) : whole_rows;
+        best.slots = (int)slots;
+        best.on = cut;
+        best.q_split = q;
+      }
+      if (slots * heads * q > 2 * UNITS) break;
     }
   }
   return best;
@@ -99,7 +106,7 @@ bool pieces(const LinattnView& v, int dtype) {
 
 template <bool OUT, bool VEC>
 void launch_walk(int dtype, int n, const LinattnArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(((long long)a.slots * a.kv_heads + 7) / 8 * 8 * a.roles));
+  const dim3 grid((unsigned)(((long long)a.slots * a.kv_heads * a.q_split + 7) / 8 * 8 * a.roles));
 #define JM_WALK(N)                                                                                              \
   if (dtype == MADE_BF16) hipLaunchKernelGGL((linattn_walk_bf16_kernel<N, OUT, VEC>), grid, dim3(128 * N), 0, s, a); \
   else hipLaunchKernelGGL((linattn_walk_f32_kernel<N, OUT, VEC>), grid, dim3(64 * N), 0, s, a)
@@ -134,6 +141,7 @@ LinattnArgs common(const linattn_config& c, const float* log_decay, const Split&
   a.B = c.B;
   a.T = c.T;
   a.kv_heads = c.kv_heads;
+  a.q_split = 1;
   a.seg_rows = s.rows;
   a.slots = s.slots;
   return a;
@@ -153,7 +161,7 @@ int take_workspace(const char* who, const linattn_config& c, void* workspace, in
 }
 
 int check_grid(const char* who, const linattn_config& c, const Split& s, int roles) {
-  if (((long long)s.slots * c.kv_heads + 7) * roles > 0x7fffffffLL || (long long)c.B * roles > 65535)
+  if (((long long)s.slots * c.kv_heads * s.q_split + 7) * roles > 0x7fffffffLL || (long long)c.B * roles > 65535 || c.kv_heads > 65535)
     return fail(MADE_ERR_ARG, "%s: B=%d, heads=%d are more than one launch takes", who, c.B, c.kv_heads);
   return MADE_OK;
 }
@@ -202,6 +210,8 @@ extern "C" int linattn_forward(const linattn_config* cfg, const void* q, const v
     launch_walk(c.dtype, a, false, s);
     launch_join(a, s);
   }
+  // (a state replaced in place is read by every workgroup that walks the whole sequence)
+  if (split.on || !state_out || state_out != state_in) a.q_split = split.q_split;
   launch_walk(c.dtype, a, true, s);
   HIP_TRY(hipGetLastError());
   return MADE_OK;
@@ -311,7 +321,7 @@ extern "C" int linattn_step(const linattn_config* cfg, const void* q, const void
   a.vec = (uintptr_t)state % 16 == 0 && c.Dv % 4 == 0;
   const long long units = (long long)c.B * c.kv_heads;
   // whole rows of the state (512 bytes) in one workgroup where there are enough of them to fill the device
-  const bool wide = units >= 2 * UNITS && c.Dv > 32;
+  const bool wide = units >= 2 * UNITS && c.Dv > 64;
   const long long grid = units * (wide ? (c.Dv + 127) / 128 : (c.Dv + 31) / 32);
   if (grid > 0x7fffffffLL) return fail(MADE_ERR_ARG, "%s: B=%d, heads=%d are more than one launch takes", who, c.B, c.kv_heads);
   hipStream_t s = (hipStream_t)stream;

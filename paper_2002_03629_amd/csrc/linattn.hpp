@@ -59,6 +59,7 @@ struct LinattnArgs {
   const int* offsets;   // [B + 1] or NULL
   int B, T, kv_heads;
   int roles;
+  int q_split;          // workgroups that share the query heads of a state (each walks the state; roles with gq > 1)
   int seg_rows;         // rows of a segment (a multiple of the block)
   int slots;            // segments in all (packed: an upper bound)
 };
@@ -204,6 +205,7 @@ __device__ __forceinline__ T la_element(const LinattnView& x, long long first, i
 struct LinattnPlace {
   LinattnSegment s;
   int which, head, p0, p1;       // role, state head, positions in the order of the walk
+  int q0, gq;                    // first of this workgroup's query heads, their number
   long long first;               // row of position 0
   long long state_at, seg_at;    // the sequence's state, the segment's place in the workspace (elements)
   float g2;                      // log2 lambda
@@ -213,10 +215,12 @@ struct LinattnPlace {
 // one XCD's L2 sees all of them.
 __device__ __forceinline__ bool la_place(const LinattnArgs& a, bool out, LinattnPlace& w) {
   const int id = blockIdx.x, pack = 8 * a.roles;
-  const int unit = id / pack * 8 + id % 8;
+  const int part = id / pack * 8 + id % 8, unit = part / a.q_split;
   w.which = id % pack / 8;
   if (unit >= a.slots * a.kv_heads) return false;
   w.head = unit % a.kv_heads;
+  w.gq = a.role[w.which].gq / a.q_split;
+  w.q0 = w.head * a.role[w.which].gq + part % a.q_split * w.gq;
   const int slot = unit / a.kv_heads;
   LinattnSegment s;
   if (!la_find(a, slot, s)) return false;
@@ -243,7 +247,7 @@ __device__ __forceinline__ const float* la_state_in(const LinattnRole& R, const 
   return R.seg && w.s.count > 1 ? R.seg + w.seg_at : R.start ? R.start + w.state_at : nullptr;
 }
 __device__ __forceinline__ float* la_state_out(const LinattnRole& R, const LinattnPlace& w, bool out) {
-  return !out ? R.seg + w.seg_at : R.end && w.s.index == w.s.count - 1 ? R.end + w.state_at : nullptr;
+  return !out ? R.seg + w.seg_at : R.end && w.s.index == w.s.count - 1 && w.q0 == w.head * R.gq ? R.end + w.state_at : nullptr;
 }
 
 // The lane's number, formed anew: what is made of it need not be kept from one use to the next.
@@ -367,7 +371,7 @@ __global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_ker
   const LinattnRole& R = a.role[w.which];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int cl = lane & 15, g = lane >> 4;
-  const int late = R.back, head = w.head, gq = R.gq, gk = R.gk;
+  const int late = R.back, head = w.head, gq = w.gq, gk = R.gk;
   const int dk = R.dk, dv = R.dv, st_r = R.st_r, parts = R.parts;
   const float g2 = w.g2;
 
@@ -397,7 +401,7 @@ __global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_ker
 
   const bool mine = 16 * wave < dv;            // this wave has values
   const int stages = gq > gk ? gq : gk;
-  const auto q_head = [&](int st) { return head * gq + (gq > 1 ? st : 0); };
+  const auto q_head = [&](int st) { return w.q0 + (gq > 1 ? st : 0); };
   const auto k_head = [&](int st) { return head * gk + (gk > 1 ? st : 0); };
   // The next block's pieces, always into the same registers: what a stage does not need is asked for from nowhere (a branch
   // around the loads would have their results moved, and so waited for, where it ends).  Groups of 4 rows of k, then of v:
@@ -699,7 +703,7 @@ __global__ __launch_bounds__(64 * N, 2) void linattn_walk_f32_kernel(LinattnArgs
   const LinattnRole& R = a.role[w.which];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int cl = lane & 31, hh = lane >> 5;
-  const int late = R.back, head = w.head, gq = R.gq, gk = R.gk;
+  const int late = R.back, head = w.head, gq = w.gq, gk = R.gk;
   const int dk = R.dk, dv = R.dv, st_r = R.st_r;
   const float g2 = w.g2;
 
@@ -731,7 +735,7 @@ __global__ __launch_bounds__(64 * N, 2) void linattn_walk_f32_kernel(LinattnArgs
 
   const bool mine = 32 * wave < dv;            // this wave has values
   const int stages = gq > gk ? gq : gk;
-  const auto q_head = [&](int st) { return head * gq + (gq > 1 ? st : 0); };
+  const auto q_head = [&](int st) { return w.q0 + (gq > 1 ? st : 0); };
   const auto k_head = [&](int st) { return head * gk + (gk > 1 ? st : 0); };
   constexpr int PERK = (KT + VT - 1) / VT;
   la_u32x4 qs[PERK][4], ks[PERK][4], vs[1][4];
@@ -901,15 +905,18 @@ __global__ __launch_bounds__(256) void linattn_join_kernel(LinattnArgs a) {
   float* p = R.seg + ((long long)slot * a.kv_heads + head) * n + i;
   const long long stride = (long long)a.kv_heads * n;
   float run = R.start ? R.start[((long long)b * a.kv_heads + head) * n + i] : 0.0f;
-  float sum = p[0];
-  for (int m = 0; m < count - 1; ++m) {
-    const float next = m + 1 < count - 1 ? p[stride] : 0.0f;
-    *p = run;
-    run = f * run + sum;
-    sum = next;
-    p += stride;
+  // (eight sums are asked for at once: one after the other they would cost a memory's latency each)
+  for (int m0 = 0; m0 < count; m0 += 8) {
+    float sum[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = m0 + e < count - 1 ? p[e * stride] : 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (m0 + e < count) p[e * stride] = run;
+      run = f * run + sum[e];
+    }
+    p += 8 * stride;
   }
-  *p = run;
 }
 
 // ------------------------------------------------------------------------------------------------------------------
