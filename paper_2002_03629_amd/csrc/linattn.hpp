@@ -533,9 +533,8 @@ __global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_ker
         if (new_q && mine) {
           const int lane = la_lane_id();
           // (la_row_swizzle(16 it + c) = la_row_swizzle(c))
-          const unsigned char* q_ = lds.q + (lane & 15) * (KT * 64);
-          const int qsw = ((lane >> 4) ^ la_row_swizzle<KT>(lane & 15)) * 16;
-          auto q_frag = [&](int it, int kb) { return *(const la_u32x4*)(q_ + (qsw ^ 64 * kb) + it * 16 * KT * 64); };
+          const int qat = (lane & 15) * (KT * 64) + ((lane >> 4) ^ la_row_swizzle<KT>(lane & 15)) * 16;
+          auto q_frag = [&](int it, int kb) { return *(const la_u32x4*)(lds.q + (qat ^ 64 * kb) + it * 16 * KT * 64); };
           // O^T = S^T Q^T: the accumulator of the state is an operand as it lies
           la_u32x4 qf[2][4];
 #pragma unroll
@@ -569,12 +568,10 @@ __global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_ker
       }
       if (!mine) continue;
       const int lane = la_lane_id(), cl = lane & 15, g = lane >> 4;
-      // (la_swizzle(16 t + c) = la_swizzle(c) ^ t for c < 16)
-      const unsigned char* kt_ = lds.kt + cl * 128;
-      const unsigned char* vt_ = lds.vt + (16 * wave + cl) * 128;
-      const int ksw = (g ^ la_swizzle(cl)) * 16, vsw = (g ^ la_swizzle(16 * wave + cl)) * 16;
-      auto v_frag = [&](int kb) { return *(const la_u32x4*)(vt_ + (vsw ^ 64 * kb)); };
-      auto kt_frag = [&](int t, int kb) { return *(const la_u32x4*)(kt_ + (ksw ^ 16 * (4 * kb ^ (t & 7))) + t * 16 * 128); };
+      // (la_swizzle(16 t + c) = la_swizzle(c) ^ t for c < 16; a column is 128 bytes: exchanging units changes its low bits alone)
+      const int kat = cl * 128 + (g ^ la_swizzle(cl)) * 16, vat = (16 * wave + cl) * 128 + (g ^ la_swizzle(16 * wave + cl)) * 16;
+      auto v_frag = [&](int kb) { return *(const la_u32x4*)(lds.vt + (vat ^ 64 * kb)); };
+      auto kt_frag = [&](int t, int kb) { return *(const la_u32x4*)(lds.kt + (kat ^ 16 * (4 * kb ^ (t & 7))) + t * 16 * 128); };
       if (OUT) {
         // O^T += V^T P^T
         la_u32x4 pf[2][6], vf[2];
