@@ -31,7 +31,7 @@ extern "C" {
 enum { ADAMW_BLOCK = 256 };
 
 typedef struct adamw_config {
-  double lr, beta1, beta2, eps, weight_decay;   /* finite; 0 <= beta < 1, eps >= 0 (0: NaN where v is 0)                */
+  double lr, beta1, beta2, eps, weight_decay;   /* finite; 0 <= beta < 1; eps a normal fp32 number or 0 (NaN where v is 0) */
   double grad_scale;                            /* factor of the gradients (1, or a clipping or loss-scaling factor)  */
   int32_t step;                                 /* 1, 2, ...: steps taken including this one                          */
   int32_t param_dtype, grad_dtype;              /* MADE_F32 or MADE_BF16 (bf16 weights are rounded to nearest)         */
@@ -40,7 +40,7 @@ typedef struct adamw_config {
 
 /*
  * adamw_step -- one step of n tensors.
- *   sizes   : elements of each tensor (0 allowed);   params, grads, m, v: n device pointers each
+ *   sizes   : elements of each tensor (0 allowed, at most 2^36 - 2^12);   params, grads, m, v: n device pointers each
  *   m_scale, v_scale: n device pointers to ceil(size / ADAMW_BLOCK) fp32 scales each (8-bit moments, else NULL)
  *   copies  : n device pointers to bf16 tensors that get the new weights rounded, or NULL; with fp32 weights only
  *   scalars : DEVICE double[4] {lr, c1, c2, grad_scale} read when the step runs, in place of cfg's lr, step and grad_scale

@@ -1,4 +1,5 @@
 // Host side of the optimiser's entry points (include/jacobi_adamw.h).
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 
@@ -11,6 +12,8 @@ namespace {
 
 typedef void (*AdamwKernel)(AdamwArgs);
 
+constexpr unsigned long long MAX_CHUNKS = 0xffffffffULL / AW_THREADS;      // of a launch: fewer than 2^32 threads
+
 // Launches `kernel` over the tensors, as many at a time as a launch's arguments hold.
 template <typename Fill>
 int launch_tensors(AdamwKernel kernel, AdamwArgs& a, int32_t n, const int64_t* sizes, hipStream_t s, Fill fill) {
@@ -18,7 +21,7 @@ int launch_tensors(AdamwKernel kernel, AdamwArgs& a, int32_t n, const int64_t* s
   unsigned long long chunks = 0;
   for (int32_t i = 0; i <= n; ++i) {
     const unsigned long long mine = i < n ? ((unsigned long long)sizes[i] + AW_CHUNK - 1) / AW_CHUNK : 0;
-    if (a.count > 0 && (i == n || a.count == AW_TENSORS || chunks + mine > 0x7fffffffULL)) {
+    if (a.count > 0 && (i == n || a.count == AW_TENSORS || chunks + mine > MAX_CHUNKS)) {
       a.first[a.count] = (unsigned)chunks;
       hipLaunchKernelGGL(kernel, dim3((unsigned)chunks), dim3(AW_THREADS), 0, s, a);
       HIP_TRY(hipGetLastError());
@@ -39,7 +42,7 @@ int check_sizes(const char* who, int32_t n, const int64_t* sizes) {
   if (n < 0) return fail(MADE_ERR_ARG, "%s: n=%d", who, n);
   if (n > 0 && !sizes) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
   for (int32_t i = 0; i < n; ++i)
-    if (sizes[i] < 0 || sizes[i] > (1LL << 42)) return fail(MADE_ERR_ARG, "%s: tensor %d has %lld elements", who, i, (long long)sizes[i]);
+    if (sizes[i] < 0 || (unsigned long long)sizes[i] > MAX_CHUNKS * AW_CHUNK) return fail(MADE_ERR_ARG, "%s: tensor %d has %lld elements", who, i, (long long)sizes[i]);
   return MADE_OK;
 }
 
@@ -52,7 +55,7 @@ extern "C" int adamw_step(const adamw_config* cfg, int32_t n, const int64_t* siz
   if (!cfg) return fail(MADE_ERR_ARG, "%s: NULL config", who);
   const adamw_config& c = *cfg;
   if (!(c.beta1 >= 0 && c.beta1 < 1 && c.beta2 >= 0 && c.beta2 < 1)) return fail(MADE_ERR_ARG, "%s: beta1=%g, beta2=%g must be in [0, 1)", who, c.beta1, c.beta2);
-  if (!(c.eps >= 0) || !std::isfinite(c.eps) || !std::isfinite(c.weight_decay)) return fail(MADE_ERR_ARG, "%s: eps=%g, weight_decay=%g", who, c.eps, c.weight_decay);
+  if (!(c.eps == 0 || (c.eps >= FLT_MIN && c.eps <= FLT_MAX)) || !std::isfinite(c.weight_decay)) return fail(MADE_ERR_ARG, "%s: eps=%g, weight_decay=%g", who, c.eps, c.weight_decay);
   if (!scalars && (!std::isfinite(c.lr) || !std::isfinite(c.grad_scale) || c.step < 1))
     return fail(MADE_ERR_ARG, "%s: lr=%g, grad_scale=%g, step=%d", who, c.lr, c.grad_scale, c.step);
   const bool p16 = c.param_dtype == MADE_BF16, g16 = c.grad_dtype == MADE_BF16;

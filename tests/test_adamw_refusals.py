@@ -32,6 +32,19 @@ def test_bad_numbers(bad):
     assert "adamw_step" in B.made_last_error()
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("eps", [1e-40, 1e-300, 1e39])
+def test_eps_that_is_no_normal_fp32_number(eps, bits):
+    """rounded to fp32 it would be zero, or its reciprocal or itself infinite"""
+    assert call(config(eps=eps, moment_bits=bits)) == B.MADE_ERR_ARG
+    assert "eps" in B.made_last_error()
+
+
+def test_a_tensor_of_more_than_a_launch_takes():
+    assert call(config(), sizes=((1 << 36),)) == B.MADE_ERR_ARG
+    assert "elements" in B.made_last_error()
+
+
 def test_bad_arguments():
     assert call(None) == B.MADE_ERR_ARG
     assert call(config(), n=-1) == B.MADE_ERR_ARG
