@@ -25,12 +25,14 @@
  * Calls are enqueued on `stream` (a hipStream_t, NULL = default stream) and return without waiting for the device; they
  * may be recorded into a graph.  The return value is MADE_OK or a negative made_status (jacobi_made.h),
  * made_last_error() has the message.  No call allocates memory.
- * Limits: 1 <= Dk, Dv <= 128; B, T >= 0.  Inputs are finite: the steps of a block of 64 (fp32: 32) are products of the
- * whole block, and a NaN or infinity in it can reach every output row of its block, earlier ones too.
+ * Limits: 1 <= Dk, Dv <= 128; B >= 0, 0 <= T <= 2^30, and a launch's workgroups have fewer than 2^32 threads together
+ * (bf16, a width above 64: 8 million states, 2.7 million for gradients; a step: 16 million parts of 32 or 128 values).
+ * Inputs are finite: the steps of a block of 64 (fp32: 32) are products of the whole block, and a NaN or infinity in it
+ * can reach every output row of its block, earlier ones too.
  *
  * Arithmetic: states, decays and sums are fp32.  MADE_F32: products are fp32.  MADE_BF16: products of bf16 values with
- * fp32 sums; the scores q_t k_s and the state a block reads are rounded to bf16 as operands of the second product, as
- * the outputs are (the state that is carried on is not).
+ * fp32 sums; scores, states and decayed values enter them as sums of two bf16 parts (2^-17 of each; three parts, 2^-25,
+ * where a state is asked for), and only the outputs are rounded to bf16.  States beyond 2^117 may overflow.
  */
 #ifndef JACOBI_LINATTN_H
 #define JACOBI_LINATTN_H

@@ -399,11 +399,13 @@ def rnn_param_grads(z, h, x, d, h0, B: int, T: int, H: int, I: int, dW, dU, db, 
 # the steps may lie further apart (parts of a wider tensor).  States and log_decay are float32.
 # ------------------------------------------------------------------------------------------------
 def _on_device(t, what: str, stream=None):
-    """A tensor that a kernel on the current device (of `stream`, if one is given) may be handed."""
+    """A tensor that a kernel on the current device may be handed, on `stream` if one is given."""
     import torch
     if not t.is_cuda:
         raise ValueError(f"{what} is not on the GPU")
-    device = torch.cuda.current_device() if stream is None else stream.device.index
+    device = torch.cuda.current_device()
+    if stream is not None and stream.device.index != device:
+        raise ValueError(f"the stream is of cuda:{stream.device.index}, the current device is cuda:{device}")
     if t.device.index != device:
         raise ValueError(f"{what} is on cuda:{t.device.index}, the call is for cuda:{device}")
     return t
@@ -445,21 +447,19 @@ def _rows(t, what: str, lead, heads: int, D: int, dtype, stream=None):
     return t.data_ptr(), ld
 
 
-def _linattn_dtype(q) -> int:
+def _linattn_dtype(dtype) -> int:
     import torch
-    if q.dtype == torch.float32:
+    if dtype == torch.float32:
         return MADE_F32
-    if q.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return MADE_BF16
-    raise ValueError(f"expected torch.float32 or torch.bfloat16, got {q.dtype}")
+    raise ValueError(f"expected torch.float32 or torch.bfloat16, got {dtype}")
 
 
 def linattn_workspace_bytes(B: int, T: int, heads: int, kv_heads: int, Dk: int, Dv: int, dtype, packed: bool = False,
                             backward: bool = False) -> int:
     """dtype: torch.float32 or torch.bfloat16."""
-    import torch
-    cfg = linattn_config(int(B), int(T), int(heads), int(kv_heads), int(Dk), int(Dv),
-                         MADE_BF16 if dtype == torch.bfloat16 else MADE_F32, 1.0, 0, 0, 0, 0, 1 if packed else None)
+    cfg = linattn_config(int(B), int(T), int(heads), int(kv_heads), int(Dk), int(Dv), _linattn_dtype(dtype), 1.0, 0, 0, 0, 0, 1 if packed else None)
     out = C.c_int64()
     _check(lib().linattn_workspace_bytes(C.byref(cfg), 1 if backward else 0, C.byref(out)))
     return out.value
@@ -469,7 +469,7 @@ def _linattn_args(q, k, v, log_decay, offsets, B, T, heads, kv_heads, Dk, Dv, sc
     import torch
     lead = (B, T) if offsets is None else (T,)
     dt = q.dtype
-    code = _linattn_dtype(q)
+    code = _linattn_dtype(q.dtype)
     pq, lq = _rows(q, "q", lead, heads, Dk, dt, stream)
     pk, lk = _rows(k, "k", lead, kv_heads, Dk, dt, stream)
     pv, lv = _rows(v, "v", lead, kv_heads, Dv, dt, stream)
@@ -527,12 +527,13 @@ def linattn_backward(q, k, v, log_decay, state_in, offsets, d_o, d_state_out, B:
 
 class PreparedLinattnStep:
     """linattn_step with its arguments marshalled once, for loops that generate step after step on the same buffers: calling
-    the object runs the step.  The tensors are kept alive; their contents may change between calls."""
+    the object runs the step, on the stream given (None: the one that is current when the object is made).  The tensors are
+    kept alive; their contents may change between calls."""
 
     def __init__(self, q, k, v, log_decay, state, slots, B: int, heads: int, kv_heads: int, Dk: int, Dv: int, scale: float, o,
                  stream=None):
         import torch
-        code = _linattn_dtype(q)
+        code = _linattn_dtype(q.dtype)
         pq, lq = _rows(q, "q", (B,), heads, Dk, q.dtype, stream)
         pk, lk = _rows(k, "k", (B,), kv_heads, Dk, q.dtype, stream)
         pv, lv = _rows(v, "v", (B,), kv_heads, Dv, q.dtype, stream)
@@ -631,7 +632,7 @@ class PreparedAdamW:
         import torch
         c = self._cfg
         c.lr, c.beta1, c.beta2, c.eps, c.weight_decay, c.grad_scale, c.step = lr, beta1, beta2, eps, weight_decay, grad_scale, step
-        if self._device.index != (torch.cuda.current_device() if stream is None else stream.device.index):
+        if any(self._device.index != d for d in (torch.cuda.current_device(), *([] if stream is None else [stream.device.index]))):
             raise ValueError(f"the tensors are on {self._device}, the call is for another device")
         _check(self._fn(C.byref(c), self._n, self._sizes, *self._arrays, _dense(scalars, "scalars", (4,), torch.float64, stream),
                         _stream(stream)))

@@ -13,12 +13,14 @@ using namespace jm;
 namespace {
 
 constexpr int UNITS = 256;      // compute units of the device
+constexpr int MAX_T = 1 << 30;                    // positions and the ends of segments behind them stay below 2^31
+constexpr long long MAX_THREADS = 0xffffffffLL;   // of a launch
 
 int block_rows(const linattn_config& c) { return c.dtype == MADE_BF16 ? LA_BF16_ROWS : LA_F32_ROWS; }
 
 int check(const char* who, const linattn_config* c, bool step) {
   if (!c) return fail(MADE_ERR_ARG, "%s: NULL config", who);
-  if (c->B < 0 || (!step && c->T < 0)) return fail(MADE_ERR_ARG, "%s: B=%d, T=%d out of range", who, c->B, c->T);
+  if (c->B < 0 || (!step && (c->T < 0 || c->T > MAX_T))) return fail(MADE_ERR_ARG, "%s: B=%d, T=%d out of range", who, c->B, c->T);
   if (c->Dk < 1 || c->Dv < 1 || c->Dk > LA_MAX_D || c->Dv > LA_MAX_D)
     return fail(MADE_ERR_ARG, "%s: Dk=%d, Dv=%d, widths of 1 to %d are supported", who, c->Dk, c->Dv, LA_MAX_D);
   if (c->kv_heads < 1 || c->heads < 1 || c->heads % c->kv_heads != 0)
@@ -55,14 +57,15 @@ int tiles(int d) { return d <= 32 ? 1 : d <= 64 ? 2 : 4; }
 Split choose(const linattn_config& c, bool backward) {
   const int C = block_rows(c);
   const long long blocks = ((long long)c.T + C - 1) / C;     // of the longest sequence there may be
-  const int whole_rows = (int)std::min<long long>(std::max<long long>(blocks, 1) * C, 0x7fffffff / C * C);
+  const int whole_rows = (int)(std::max<long long>(blocks, 1) * C);
   Split best = {whole_rows, c.B, false, 1};
   const int group = c.heads / c.kv_heads;
   const double size = (c.dtype == MADE_BF16 ? 1.0 : 1.55) * (0.55 + 0.45 * tiles(c.Dk) * tiles(c.Dv) / 16.0);
   const double sums = size * 1.9 * (backward ? 0.5 * (1 + group) : 1.0), heads = (double)c.kv_heads;
   auto turns = [](double n) { return n <= UNITS ? 1.0 : 1.7 * std::ceil(n / (2 * UNITS)); };
   double least = 1e300;
-  // (segments about an eighth apart in number; all divisors of a group are tried, whose passes each walk the state again)
+  // (numbers of segments about an eighth apart; the heads of a group may be shared out, each part then walks the state again,
+  // but not among more workgroups than run at once)
   for (long long m = 1, last = 0; m <= std::max<long long>(blocks, 1) && m <= 1 << 20; m += std::max<long long>(1, m / 8)) {
     const long long L = std::max<long long>(1, (blocks + m - 1) / m);
     if (L == last) continue;
@@ -71,7 +74,7 @@ Split choose(const linattn_config& c, bool backward) {
     const double slots = !cut ? c.B : c.offsets ? (double)(blocks / L + c.B) : (double)((blocks + L - 1) / L) * c.B;
     const double states = slots * heads * c.Dk * c.Dv * 4.0 * (backward ? 2 : 1);
     const double extra = !cut ? 0.0 : turns(slots * heads * (backward ? 2 : 1)) * (sums * (double)L + 2.0) + states * 3.0 / 5e6 + 8.0;
-    for (int q = 1; q <= (backward ? 1 : group); ++q) {
+    for (int q = 1; q <= (backward ? 1 : group) && (q == 1 || slots * heads * q <= 2 * UNITS); ++q) {
       if (group % q != 0) continue;
       const double walk = size * (4.4 + 3.2 * (group / q - 1));
       const double cost = turns(slots * heads * q * (backward ? 3 : 1)) * (walk * (double)L + 4.0) + extra;
@@ -82,7 +85,6 @@ Split choose(const linattn_config& c, bool backward) {
         best.on = cut;
         best.q_split = q;
       }
-      if (slots * heads * q > 2 * UNITS) break;
     }
   }
   return best;
@@ -153,7 +155,7 @@ int take_workspace(const char* who, const linattn_config& c, void* workspace, in
   const long long need = state_floats(c, split) * 4 * sets;
   if (split.on && (!workspace || bytes < need)) {
     const int C = block_rows(c);
-    split.rows = (int)std::min<long long>(((long long)c.T + C - 1) / C * C, 0x7fffffff / C * C);
+    split.rows = (int)(((long long)c.T + C - 1) / C * C);
     split.slots = c.B;
     split.on = false;
   }
@@ -161,7 +163,9 @@ int take_workspace(const char* who, const linattn_config& c, void* workspace, in
 }
 
 int check_grid(const char* who, const linattn_config& c, const Split& s, int roles) {
-  if (((long long)s.slots * c.kv_heads * s.q_split + 7) * roles > 0x7fffffffLL || (long long)c.B * roles > 65535 || c.kv_heads > 65535)
+  const int n = tiles(std::max(c.Dk, c.Dv));
+  const long long units = (long long)s.slots * c.kv_heads * s.q_split + 7;
+  if (units * roles > MAX_THREADS / ((c.dtype == MADE_BF16 ? 128 : 64) * n) || (s.on && ((long long)c.B * roles > 65535 || c.kv_heads > 65535)))
     return fail(MADE_ERR_ARG, "%s: B=%d, heads=%d are more than one launch takes", who, c.B, c.kv_heads);
   return MADE_OK;
 }
@@ -183,6 +187,7 @@ extern "C" int linattn_forward(const linattn_config* cfg, const void* q, const v
   const linattn_config& c = *cfg;
   if (c.B == 0) return MADE_OK;
   if (!log_decay || (c.T > 0 && (!q || !k || !v || !o))) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
+  if (o && (o == q || o == k || o == v)) return fail(MADE_ERR_ARG, "%s: o is one of the inputs", who);
   Split split = choose(c, false);
   TRY(take_workspace(who, c, workspace, workspace_bytes, 1, split));
   TRY(check_grid(who, c, split, 1));
@@ -226,6 +231,12 @@ extern "C" int linattn_backward(const linattn_config* cfg, const void* q, const 
   if (c.B == 0) return MADE_OK;
   if (!log_decay || (c.T > 0 && (!q || !k || !v || !d_o || !dq || !dk || !dv))) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
   if (d_state_in && d_state_in == d_state_out) return fail(MADE_ERR_ARG, "%s: d_state_in is d_state_out", who);
+  const void *in[4] = {q, k, v, d_o}, *out[3] = {dq, dk, dv};
+  for (int i = 0; i < 3; ++i) {
+    for (int j = 0; j < 4; ++j)
+      if (out[i] && out[i] == in[j]) return fail(MADE_ERR_ARG, "%s: a gradient is one of the inputs", who);
+    if (out[i] && out[i] == out[(i + 1) % 3]) return fail(MADE_ERR_ARG, "%s: two gradients are one array", who);
+  }
   Split split = choose(c, true);
   TRY(take_workspace(who, c, workspace, workspace_bytes, 2, split));
   TRY(check_grid(who, c, split, 3));
@@ -303,6 +314,7 @@ extern "C" int linattn_step(const linattn_config* cfg, const void* q, const void
   if (n_slots < 0 || (!slots && n_slots < c.B)) return fail(MADE_ERR_ARG, "%s: n_slots=%d, B=%d", who, n_slots, c.B);
   if (c.B == 0) return MADE_OK;
   if (!q || !k || !v || !log_decay || !state || !o) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
+  if (o == q || o == k || o == v) return fail(MADE_ERR_ARG, "%s: o is one of the inputs", who);
   LinattnStepArgs a;
   a.q = view(q, c.ld_q, c.heads, c.Dk);
   a.k = view(k, c.ld_k, c.kv_heads, c.Dk);
@@ -323,7 +335,7 @@ extern "C" int linattn_step(const linattn_config* cfg, const void* q, const void
   // whole rows of the state (512 bytes) in one workgroup where there are enough of them to fill the device
   const bool wide = units >= 2 * UNITS && c.Dv > 64;
   const long long grid = units * (wide ? (c.Dv + 127) / 128 : (c.Dv + 31) / 32);
-  if (grid > 0x7fffffffLL) return fail(MADE_ERR_ARG, "%s: B=%d, heads=%d are more than one launch takes", who, c.B, c.kv_heads);
+  if (grid > MAX_THREADS / 256) return fail(MADE_ERR_ARG, "%s: B=%d, heads=%d are more than one launch takes", who, c.B, c.kv_heads);
   hipStream_t s = (hipStream_t)stream;
 #define JM_STEP(T, COLS) hipLaunchKernelGGL((linattn_step_kernel<T, COLS>), dim3((unsigned)grid), dim3(256), 0, s, a)
   if (c.dtype == MADE_BF16) {

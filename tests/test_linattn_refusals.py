@@ -52,6 +52,59 @@ def test_null_arguments_and_workspaces():
     assert L.linattn_step(C.byref(config()), P, P, P, P, P, -1, P, P, None) == B.MADE_ERR_ARG
 
 
+def refused(code, text):
+    return code == B.MADE_ERR_ARG and text in B.made_last_error()
+
+
+def test_more_than_a_launch_takes():
+    """T beyond 2^30; workgroups of 2^32 threads together (bf16, widths of 128: 512 each; a step's have 256)"""
+    L, q = B.lib(), [C.c_void_p(4096 * (i + 1)) for i in range(12)]
+    out = C.c_int64()
+    for T in ((1 << 30) + 1, (1 << 31) - 1):
+        assert refused(L.linattn_workspace_bytes(C.byref(config(T=T)), 0, C.byref(out)), "T=")
+        assert refused(L.linattn_forward(C.byref(config(T=T)), *q[:4], None, q[4], None, None, 0, None), "T=")
+    assert L.linattn_workspace_bytes(C.byref(config(T=1 << 30)), 0, C.byref(out)) == B.MADE_OK and out.value > 0
+    wide = config(B=1 << 23, T=1, heads=1, kv_heads=1, Dk=128, Dv=128)
+    assert refused(L.linattn_forward(C.byref(wide), *q[:4], None, q[4], None, None, 0, None), "launch")
+    wide.B = 3 << 20
+    assert refused(L.linattn_backward(C.byref(wide), *q[:4], None, q[4], None, *q[5:8], None, None, 0, None), "launch")
+    wide.B = 1 << 24
+    assert refused(L.linattn_step(C.byref(wide), *q[:5], 1 << 24, None, q[5], None), "launch")
+
+
+def test_an_output_that_is_an_input():
+    L, q = B.lib(), [C.c_void_p(4096 * (i + 1)) for i in range(12)]
+    for i in range(3):
+        assert refused(L.linattn_forward(C.byref(config()), *q[:4], None, q[i], None, None, 0, None), "inputs")
+        assert refused(L.linattn_step(C.byref(config()), *q[:5], 2, None, q[i], None), "inputs")
+        for j in (0, 1, 2, 4):
+            grads = q[5:8]
+            grads[i] = q[j]
+            assert refused(L.linattn_backward(C.byref(config()), *q[:4], None, q[4], None, *grads, None, None, 0, None), "inputs")
+        grads = q[5:8]
+        grads[i] = grads[i - 1]
+        assert refused(L.linattn_backward(C.byref(config()), *q[:4], None, q[4], None, *grads, None, None, 0, None), "two gradients")
+
+
+def test_the_binding_refuses_other_types():
+    with pytest.raises(ValueError, match="float16"):
+        B.linattn_workspace_bytes(1, 64, 4, 2, 16, 16, torch.float16)
+
+
+def test_the_binding_refuses_a_stream_of_another_device(monkeypatch):
+    class Of:
+        is_cuda = True
+
+        def __init__(self, index):
+            self.device = torch.device("cuda", index)
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    assert B._on_device(Of(0), "x") and B._on_device(Of(0), "x", Of(0))
+    for t, s in ((1, None), (1, 0), (1, 1), (0, 1)):
+        with pytest.raises(ValueError, match="cuda:1"):
+            B._on_device(Of(t), "x", None if s is None else Of(s))
+
+
 def test_an_empty_batch_needs_no_pointers():
     L = B.lib()
     c = C.byref(config(B=0))
