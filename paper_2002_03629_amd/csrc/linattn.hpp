@@ -6,8 +6,8 @@
 //     o_i = scale ( lambda^(i+1) S^T q_i + sum_{j <= i} lambda^(i-j) (q_i . k_j) v_j )
 //     S  <- lambda^C S + sum_j lambda^(C-1-j) k_j v_j^T
 // which is four matrix products.  One workgroup owns the state of one head for a run of steps (a segment) and walks its
-// blocks of C steps: the state stays in accumulator registers, wave w holds its value columns 32 w .. 32 w + 31, the
-// block's q, k, v pass through LDS, the next block's are requested before the products of this one.
+// blocks of C steps: the state stays in accumulator registers, divided among the waves by value columns, the block's q, k, v
+// pass through LDS, the next block's are requested before the products of this one.
 //
 // The gradients are the same recurrence with the arrays in other roles, so the same kernel computes them:
 //     dq: queries do, keys v, values k, forward in time, the states of the forward pass (transposed)
@@ -26,7 +26,6 @@ typedef __attribute__((ext_vector_type(4))) uint32_t la_u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t la_u32x2;
 typedef __attribute__((ext_vector_type(4))) float la_f32x4;
 typedef __attribute__((ext_vector_type(8))) __bf16 la_bf16x8;
-typedef __attribute__((ext_vector_type(4))) __bf16 la_bf16x4;
 typedef __attribute__((ext_vector_type(8))) float la_f32x8;
 typedef __attribute__((ext_vector_type(16))) float la_f32x16;
 
@@ -49,7 +48,7 @@ struct LinattnRole {
   int st_r, st_c;       // state element (key r, value c) at r * st_r + c * st_c (dq and dk hold it transposed)
   int gq, gk;           // query heads / key heads per state (one of them is 1)
   int back;             // 1: steps are taken from the last to the first
-  int parts;            // bf16: parts the decayed values are split into for the state (1: rounded; 3: exact to fp32)
+  int parts;            // bf16: parts the decayed values are split into for the state (2, or 3 for states that leave in fp32)
   float p_scale, s_scale, i_scale;   // factors of the scores, of what enters the state, of what is read from it
 };
 
@@ -163,8 +162,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t la_buffer(const void* p, int b
 }
 
 // n rows of an operand from the row of position 0 (`first`) on, in the order of the walk.  The descriptor begins at their
-// lowest row and ends behind their highest; position p is la_row(...) bytes from its begin: what lies behind the n rows falls
-// out of it, forward above its end, back below zero.
+// lowest row and ends behind their highest; position p is la_lane + at0 bytes from its begin: what lies behind the n rows
+// falls out of it, forward above its end, back below zero.
 template <typename T>
 struct LaBlock {
   __amdgpu_buffer_rsrc_t buf;
@@ -360,8 +359,8 @@ __device__ __forceinline__ la_f32x4 la_mfma16(la_u32x4 x, la_u32x4 y, la_f32x4 c
 
 // OUT = true: the walk with outputs.  OUT = false: only the state a segment adds, from zero, into the workspace.
 // VEC: every operand's rows come in 16-byte pieces (else none is taken to).
-// The second half of the keys, and waves of values, that a role does not have are passed over, so that one kernel of N x 32 keys and values
-// serves the roles of a gradient together.
+// The second half of the keys, and waves of values, that a role does not have are passed over, so that one kernel of N x 32
+// keys and values serves the roles of a gradient together.
 template <int N, bool OUT, bool VEC>
 __global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_kernel(LinattnArgs a) {
   constexpr int C = LA_BF16_ROWS, KT = N, VT = N, NT = 128 * VT, NW = 2 * VT;
@@ -440,14 +439,14 @@ __global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_ker
   if (VEC) request(w.p0, 0);
 
   // The state in the registers is the state divided by `frame`: a block's decay goes into `frame` and only where that leaves
-  // 2^-30 .. 2^30 into the 2 KT x 4 registers.
+  // 2^-10 .. 2^10 into the 2 KT x 4 registers (fp32's range is shorter by as much).
   float frame = 1.0f;
 
   la_f32x4 O[4];
   for (int p = w.p0; p < w.p1; p += C) {
     const int n = min(C, w.p1 - p);
     const float factor = la_uniform(frame * la_pow(g2, n));
-    const bool rescale = __builtin_amdgcn_readfirstlane(!(factor >= 0x1p-30f && factor <= 0x1p30f));
+    const bool rescale = __builtin_amdgcn_readfirstlane(!(factor >= 0x1p-10f && factor <= 0x1p10f));
     const float next = la_uniform(rescale ? 1.0f : factor);
     const long long row = R.back ? w.first - p : w.first + p;
     for (int st = 0; st < stages; ++st) {
@@ -604,7 +603,7 @@ __global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_ker
           }
         }
       }
-      // S = lambda^n S + K^T V'
+      // S = lambda^n S + K^T V', the decayed values V' in two parts (one would lose as much as the outputs' own rounding) or three
       if (rescale && (gk > 1 ? st == 0 : last)) {
 #pragma unroll
         for (int t = 0; t < 2 * KT; ++t)

@@ -5,8 +5,9 @@ oracle on absolute inputs).
   * fp32 sums: every term passes at most N roundings of 2^-24: a product's sum over D, a sum over a block of 64 steps, a
     block's or a segment's step of the state (two each), the factors lambda^n (their exponent's rounding counts |n log2
     lambda|, of which at most 150 before the factor is zero) and a handful of single ones.
-  * bf16 operands of the second product: the scores, the decayed values and the state that is read are rounded once each, and
-    no term meets more than two of these roundings: 2 x 2^-8 A; the output's rounding is 2^-8 of its value.
+  * bf16 operands of the second product (two parts each, of which this allows one): the scores, the decayed values and the
+    state that is read are rounded once each, and no term meets more than two of these roundings: 2 x 2^-8 A; the output's
+    rounding is 2^-8 of its value.
 The states that leave a call are fp32 sums whatever the type of the steps.
 """
 import numpy as np
@@ -155,7 +156,7 @@ def test_widths(dtype, Dk, Dv):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("heads,kv", [(1, 1), (8, 1), (6, 2), (5, 5), (12, 4)])
+@pytest.mark.parametrize("heads,kv", [(1, 1), (8, 1), (6, 2), (5, 5), (12, 4), (16, 1), (9, 3)])
 def test_shared_states(dtype, heads, kv):
     Case(dtype, [100] * 3, heads, kv, 32, 64, seed=heads).check_all()
 
@@ -170,6 +171,41 @@ def test_decays(dtype, decay):
 @pytest.mark.parametrize("lengths", [[5, 0, 1, 130, 64], [0], [0, 0, 3], [300, 2] + [1] * 70 + [90, 0], [65] * 9])
 def test_packed(dtype, lengths):
     Case(dtype, lengths, 4, 2, 32, 64, packed=True, spare=3).check_all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_steps(dtype):
+    """sequences of no steps hand their states on"""
+    c = Case(dtype, [0] * 3, 4, 2, 64, 32)
+    o, s = c.forward()
+    assert o.numel() == 0 and torch.equal(s, c.t["s"])
+    *_, ds = c.backward()
+    assert torch.equal(ds, c.t["ds"])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e-20, 1e25])
+def test_values_far_from_one(dtype, size):
+    c = Case(dtype, [200], 2, 2, 64, 64, decay="none")
+    for key in ("v", "s"):
+        c.t[key] = (c.t[key].double() * size).to(c.t[key].dtype)
+        c.x[key] = c.t[key].double().cpu().numpy()
+    c.compare("forward", c.forward())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_bf16_outputs_are_off_by_little_more_than_their_own_rounding(dtype):
+    """Scores, states and decayed values are two bf16 parts each: 2^-17 of every term, three roundings at most, beside fp32's
+    (a bound 1.5 % above that of the output's rounding alone where A is of the output's size)."""
+    for heads, kv, decay in ((2, 2, "mixed"), (4, 1, "none")):
+        c = Case(dtype, [500], heads, kv, 128, 128, decay=decay, carry=False)
+        o, _ = c.forward(state_out=None)
+        ref, mag = c.oracle("forward", 0)[0], c.oracle("forward", 0, True)[0]
+        err = np.abs(o[0].double().cpu().numpy() - ref)
+        tol = c.roundings(500) * 2.0 ** -24 * mag
+        if dtype == "bf16":
+            tol = tol + 3 * 2.0 ** -17 * mag + 2.0 ** -8 * np.abs(ref)
+        assert (err <= tol).all()
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
