@@ -332,7 +332,8 @@ extern "C" int linattn_step(const linattn_config* cfg, const void* q, const void
   a.scale = c.scale;
   a.vec = (uintptr_t)state % 16 == 0 && c.Dv % 4 == 0;
   const long long units = (long long)c.B * c.kv_heads;
-  // whole rows of the state (512 bytes) in one workgroup where there are enough of them to fill the device
+  // whole rows of the state (512 bytes) in one workgroup where there are enough of them to fill the device (250 rows of 8
+  // states of 128 x 128: 128 columns 49.6 us, 32 columns 51.6; one row of 8 states of that size: 8.9 and 5.8)
   const bool wide = units >= 2 * UNITS && c.Dv > 64;
   const long long grid = units * (wide ? (c.Dv + 127) / 128 : (c.Dv + 31) / 32);
   if (grid > MAX_THREADS / 256) return fail(MADE_ERR_ARG, "%s: B=%d, heads=%d are more than one launch takes", who, c.B, c.kv_heads);

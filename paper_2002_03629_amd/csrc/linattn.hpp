@@ -9,6 +9,13 @@
 // blocks of C steps: the state stays in accumulator registers, divided among the waves by value columns, the block's q, k, v
 // pass through LDS, the next block's are requested before the products of this one.
 //
+// What it costs (one sequence of 32768 steps, 32 heads, widths of 128, bf16, 16 segments to a head: 412 us in all with calls in
+// a row, 1.07 GB of q, k, v and o take 221 at the 4.85 TB/s that a copy of 2 GiB reaches; a kernel trace shows each launch
+// somewhat longer than in a row): the walk 299 us, 4.6 us of a compute unit for a block's 64 KB (3.5 at the copy's rate); by
+// the counters the SIMDs issue vector instructions 54 % and run MFMAs 33 % of the time (issue cycles and busy cycles over
+// those of the shader engines), LDS is read or written 40 %.  Vector and matrix time added up in every variant timed, so fewer
+// instructions is what has paid.  The pass for the sums 133 us, 2.1 us a block's 32 KB (1.7), 51 % and 25 %.
+//
 // The gradients are the same recurrence with the arrays in other roles, so the same kernel computes them:
 //     dq: queries do, keys v, values k, forward in time, the states of the forward pass (transposed)
 //     dk: queries v, keys do, values q, back in time;     dv: queries k, keys q, values do, back in time
@@ -439,7 +446,8 @@ __global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_ker
   if (VEC) request(w.p0, 0);
 
   // The state in the registers is the state divided by `frame`: a block's decay goes into `frame` and only where that leaves
-  // 2^-10 .. 2^10 into the 2 KT x 4 registers (fp32's range is shorter by as much).
+  // 2^-10 .. 2^10 into the 2 KT x 4 registers (fp32's range is shorter by as much; multiplying every block
+  // would be 32 instructions a wave).
   float frame = 1.0f;
 
   la_f32x4 O[4];
@@ -656,6 +664,10 @@ __global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_ker
 
 // ---- fp32: blocks of 32 steps, 32 x 32 x 2 MFMA (an accumulator's rows are operand values as they lie, so nothing is turned
 // over).  Wave w holds the value columns 32 w .. 32 w + 31.
+//
+// Bound by the chain of a block's products, not by memory: 3 x 1777 steps of 6 heads, widths 72 and 100, one workgroup to a
+// unit, one wave to a SIMD: the walk 37 us (MFMAs 42 %, vector issue 11 % of the time), the pass for the sums 18, the join 5;
+// the 45 MB take 9 at the copy's rate.
 template <int KT, bool OUT>
 struct LaLdsF32 {
   static constexpr int PITCH = KT * 32 + 4, VPITCH = PITCH;
@@ -890,6 +902,7 @@ __global__ __launch_bounds__(64 * N, 2) void linattn_walk_f32_kernel(LinattnArgs
 
 // The states that enter the segments, from what each segment adds: start[0] = the sequence's first state,
 // start[m + 1] = lambda^rows start[m] + sum[m], in place.  One thread an element, grid (elements, kv heads, sequences x roles).
+// Bound by memory: 32 heads' 16 segments of 128 x 128 (2 x 33.5 MB) 15 us, 24 packed sequences' 128 segments of 8 heads 31 us.
 __global__ __launch_bounds__(256) void linattn_join_kernel(LinattnArgs a) {
   const int b = blockIdx.z % a.B, head = blockIdx.y;
   const LinattnRole& R = a.role[blockIdx.z / a.B];
@@ -938,7 +951,10 @@ constexpr int LA_STEP_GROUP = 8;   // query heads whose sums are taken at once
 
 // One workgroup takes COLS value columns of one row's state: every element is read and written once, which is all the time
 // there is to it.  A thread holds 4 columns of every (1024 / COLS)-th key; the sums over keys of q * S meet through lanes
-// and LDS.
+// and LDS.  States pass by the caches (non-temporal): between two steps of a layer those of the others come.  250 rows (some
+// without a place) of 8 states of 128 x 128, 237 MB in and out: 52.4 us with states last used long ago, 49.6 used by the call
+// before (with ordinary loads and stores 68.2 and 49.5; multiplying as many floats in place takes 47.5 and 37.1); one row
+// of 8 states of 64 x 64: 4.9 us, a launch's time.
 template <typename T, int COLS>
 __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnStepArgs a) {
   constexpr int CW = COLS / 4, RG = 256 / CW, PER = LA_MAX_D / RG;
@@ -961,7 +977,11 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnStepArgs a) {
     for (int c = 0; c < 4; ++c) x[i][c] = 0.0f;
     if (r < a.dk) {
       if (a.vec) {
-        if (c0 < a.dv) *(float4*)x[i] = *(const float4*)(base + (long long)r * a.dv);
+        if (c0 < a.dv) {
+          const la_f32x4 y = __builtin_nontemporal_load((const la_f32x4*)(base + (long long)r * a.dv));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) x[i][c] = y[c];
+        }
       } else {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -1047,7 +1067,8 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnStepArgs a) {
     const int r = rg + i * RG;
     if (r < a.dk) {
       if (a.vec) {
-        if (c0 < a.dv) *(float4*)(base + (long long)r * a.dv) = *(const float4*)x[i];
+        if (c0 < a.dv)
+          __builtin_nontemporal_store(la_f32x4{x[i][0], x[i][1], x[i][2], x[i][3]}, (la_f32x4*)(base + (long long)r * a.dv));
       } else {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
