@@ -138,6 +138,35 @@ def test_a_large_tensor(bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_a_tensor_beyond_4_gib(bits):
+    """its ends are the same as tensors of their own"""
+    part = 2 * 4096 + 5
+    n = (1 << 30) + 4096 + part + (7 << 29 if bits == 8 else 0)      # (8 bits: the codes too lie beyond 4 GiB)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    ends = [slice(0, 8192), slice(n - part, n)]
+    dt = torch.bfloat16 if bits == 8 else torch.float32
+    p, d = torch.zeros(n, dtype=dt, device="cuda"), torch.zeros(n, dtype=dt, device="cuda")
+    for e in ends:
+        p[e] = torch.randn(e.stop - e.start, generator=g, device="cuda").to(dt)
+        d[e] = torch.randn(e.stop - e.start, generator=g, device="cuda").to(dt)
+    small_p, small_d = [p[e].clone() for e in ends], [d[e].clone() for e in ends]
+    big, small = B.adamw_moments([p], bits), B.adamw_moments(small_p, bits)
+    for t in (1, 2):
+        B.adamw_step([p], [d], *big[:2], *HYPER.values(), t, *big[2:])
+        B.adamw_step(small_p, small_d, *small[:2], *HYPER.values(), t, *small[2:])
+    for i, e in enumerate(ends):
+        assert torch.equal(p[e], small_p[i])
+        for a, b in zip(big[:2], small[:2]):
+            assert torch.equal(a[0][e], b[i]) and b[i].any()
+        if bits == 8:
+            blocks = slice(e.start // 256, -(-e.stop // 256))
+            assert all(torch.equal(a[0][blocks], b[i]) for a, b in zip(big[2:], small[2:]))
+    assert not p[8192:n - part].any()
+    del p, d, big
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_hyperparameters(bits):
     for i, kw in enumerate([dict(weight_decay=0.0), dict(beta1=0.0), dict(beta2=0.0, eps=1e-3), dict(lr=0.0), dict(lr=-0.01), dict(grad_scale=0.125)]):
         t = Tensors([700], bits=bits, seed=i)

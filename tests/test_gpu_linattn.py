@@ -351,6 +351,69 @@ def test_prompt_then_single_steps(dtype):
     assert (pool[0] == 0).all() and (pool[2] == 0).all()
 
 
+@pytest.mark.parametrize("dtype,T", [("bf16", 300), ("f32", 150)])
+def test_rows_as_far_apart_as_they_may_be(dtype, T):
+    """2^23 elements from row to row: the last rows lie beyond 4 GiB, a block spans 1 GiB"""
+    c = Case(dtype, [T], 2, 2, 32, 32, wide=(1 << 23) - 64)
+    assert c.t["q"].stride(1) == 1 << 23 and c.t["q"].stride(1) * c.t["q"].element_size() * (T - 1) > 1 << 32
+    c.compare("forward", c.forward())
+    c.compare("backward", c.backward())
+    torch.cuda.empty_cache()
+
+
+def test_states_beyond_4_gib():
+    n, g = 70000, np.random.default_rng(5)
+    state = torch.zeros(n, 1, 128, 128, device="cuda")
+    slots = torch.tensor([n - 1, 3, n - 2, n - 1], dtype=torch.int32, device="cuda")
+    s0 = torch.from_numpy(g.normal(size=(3, 1, 128, 128)).astype(np.float32)).cuda()
+    places = [n - 1, 3, n - 2]
+    state[places] = s0
+    q, k, v = (torch.from_numpy(g.normal(size=(4, 1, 128)).astype(np.float32)).cuda() for _ in range(3))
+    ld, o, near, o2 = torch.full((1,), -0.1, device="cuda"), torch.empty_like(q), s0.clone(), torch.empty_like(q)
+    B.linattn_step(q, k, v, ld, state, slots, 4, 1, 1, 128, 128, 0.1, o)
+    B.linattn_step(q, k, v, ld, near, torch.tensor([0, 1, 2, 0], dtype=torch.int32, device="cuda"), 4, 1, 1, 128, 128, 0.1, o2)
+    assert torch.equal(o, o2) and torch.equal(state[places], near)
+    state[places] = 0
+    assert not state.any()
+    del state
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_more_sequences_than_a_cut_call_may_have(dtype):
+    """one block each: the last ones are the same as in a call of their own"""
+    n, T = 30000, 3
+    c = Case(dtype, [T] * n, 2, 1, 16, 16)
+    last = Case(dtype, [T] * 5, 2, 1, 16, 16)
+    for key in ("q", "k", "v", "do", "s", "ds"):
+        last.t[key].copy_(c.t[key][-5:])
+        last.x[key] = c.x[key][-5:]
+    for fn in ("forward", "backward"):
+        all_, few = getattr(c, fn)(), getattr(last, fn)()
+        last.compare(fn, few)
+        last.compare(fn, [x[-5:] for x in all_])
+
+
+def test_two_calls_at_once():
+    """on two streams, a workspace each"""
+    c = [Case("bf16", [3000], 4, 2, 64, 64, seed=i) for i in range(2)]
+    ref = [(x.forward(), x.backward()) for x in c]
+    need = [B.linattn_workspace_bytes(1, 3000, 4, 2, 64, 64, torch.bfloat16, backward=b) for b in (False, True)]
+    assert min(need) > 0
+    streams = [torch.cuda.Stream() for _ in c]
+    ws = [[torch.empty(n, dtype=torch.uint8, device="cuda") for n in need] for _ in c]
+    torch.cuda.synchronize()
+    got = [None] * 2
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = (c[i].forward(workspace=ws[i][0]), c[i].backward(workspace=ws[i][1]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for a, b in zip(ref[i], got[i]):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
 def test_captured_and_replayed():
     """forward, backward and a step in one graph, replayed on new inputs with eager work between"""
     c = Case("bf16", [400] * 2, 4, 2, 64, 64)
