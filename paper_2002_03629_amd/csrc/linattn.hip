@@ -211,12 +211,10 @@ extern "C" int linattn_forward(const linattn_config* cfg, const void* q, const v
   r.parts = state_out ? 3 : 2;
   r.p_scale = r.i_scale = c.scale;
   r.s_scale = 1.0f;
-  if (split.on) {
-    launch_walk(c.dtype, a, false, s);
-    launch_join(a, s);
-  }
-  // (a state replaced in place is read by every workgroup that walks the whole sequence)
+  if (split.on) launch_walk(c.dtype, a, false, s);
+  // (without a workspace for its copy, a state replaced in place is read by one workgroup alone: the one that writes it)
   if (split.on || !state_out || state_out != state_in) a.q_split = split.q_split;
+  if (split.on) launch_join(a, s);
   launch_walk(c.dtype, a, true, s);
   HIP_TRY(hipGetLastError());
   return MADE_OK;

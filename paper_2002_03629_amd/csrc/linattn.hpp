@@ -249,8 +249,12 @@ __device__ __forceinline__ bool la_place(const LinattnArgs& a, bool out, Linattn
   return true;
 }
 
-__device__ __forceinline__ const float* la_state_in(const LinattnRole& R, const LinattnPlace& w) {
-  return R.seg && w.s.count > 1 ? R.seg + w.seg_at : R.start ? R.start + w.state_at : nullptr;
+// Workgroups that share a state's query heads each read the state that enters, one of them writes the one that leaves, and
+// nothing orders the two: where a call replaces states in place, a sequence of one segment is read from a copy too, which
+// the join makes (q_split > 1 has at most 512 states and parts: a copy is a few us).
+__host__ __device__ __forceinline__ bool la_copied(const LinattnArgs& a, const LinattnRole& R) { return a.q_split > 1 && R.end && R.end == R.start; }
+__host__ __device__ __forceinline__ const float* la_state_in(const LinattnArgs& a, const LinattnRole& R, const LinattnPlace& w) {
+  return R.seg && (w.s.count > 1 || la_copied(a, R)) ? R.seg + w.seg_at : R.start ? R.start + w.state_at : nullptr;
 }
 __device__ __forceinline__ float* la_state_out(const LinattnRole& R, const LinattnPlace& w, bool out) {
   return !out ? R.seg + w.seg_at : R.end && w.s.index == w.s.count - 1 && w.q0 == w.head * R.gq ? R.end + w.state_at : nullptr;
@@ -386,7 +390,7 @@ __global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_ker
   const int col = 16 * wave + cl;
   const unsigned state_off = (unsigned)(4 * g * R.st_r + col * R.st_c) * 4;
   if (OUT) {
-    const float* src = la_state_in(R, w);
+    const float* src = la_state_in(a, R, w);
     const __amdgpu_buffer_rsrc_t buf = la_buffer(src);
 #pragma unroll
     for (int t = 0; t < 2 * KT; ++t)
@@ -720,7 +724,7 @@ __global__ __launch_bounds__(64 * N, 2) void linattn_walk_f32_kernel(LinattnArgs
   const int col = 32 * wave + cl;
   unsigned state_off = (unsigned)(4 * hh * R.st_r + col * R.st_c) * 4;
   if (OUT) {
-    const float* src = la_state_in(R, w);
+    const float* src = la_state_in(a, R, w);
     const __amdgpu_buffer_rsrc_t buf = la_buffer(src);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
@@ -901,7 +905,7 @@ __global__ __launch_bounds__(64 * N, 2) void linattn_walk_f32_kernel(LinattnArgs
 }
 
 // The states that enter the segments, from what each segment adds: start[0] = the sequence's first state,
-// start[m + 1] = lambda^rows start[m] + sum[m], in place.  One thread an element, grid (elements, kv heads, sequences x roles).
+// start[m + 1] = lambda^rows start[m] + sum[m], in place (of one segment: its copy, see la_copied).  One thread an element, grid (elements, kv heads, sequences x roles).
 // Bound by memory: 32 heads' 16 segments of 128 x 128 (2 x 33.5 MB) 15 us, 24 packed sequences' 128 segments of 8 heads 31 us.
 __global__ __launch_bounds__(256) void linattn_join_kernel(LinattnArgs a) {
   const int b = blockIdx.z % a.B, head = blockIdx.y;
@@ -909,7 +913,7 @@ __global__ __launch_bounds__(256) void linattn_join_kernel(LinattnArgs a) {
   const int n = R.dk * R.dv, i = blockIdx.x * 256 + threadIdx.x;
   int len;
   const int slot = la_first_slot(a, b, len), count = min(la_count(a, len), a.slots - slot);
-  if (i >= n || count < 2) return;
+  if (i >= n || count < (la_copied(a, R) ? 1 : 2)) return;
   const float f = la_pow(a.log_decay[head] * 1.44269504088896340736f, a.seg_rows);
   float* p = R.seg + ((long long)slot * a.kv_heads + head) * n + i;
   const long long stride = (long long)a.kv_heads * n;

@@ -1,0 +1,136 @@
+// Host side of the linear-attention entry points without a GPU (test code): their source is compiled for the host alone, under
+// UndefinedBehaviorSanitizer, against a stand-in for the runtime that keeps the launches in place of running them.
+#include "../paper_2002_03629_amd/csrc/linattn.hip"
+
+#include <cstdarg>
+#include <cstdio>
+#include <string>
+#include <vector>
+
+struct Launch {
+  std::string kernel;
+  dim3 grid, block;
+  LinattnArgs args;
+};
+static std::vector<std::pair<const void*, std::string>> g_names;
+static std::vector<Launch> g_launches;
+static dim3 g_grid, g_block;
+static char g_error[512];
+
+int jm::fail(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_error, sizeof g_error, fmt, ap);
+  va_end(ap);
+  return code;
+}
+
+extern "C" {
+void** __hipRegisterFatBinary(const void*) {
+  static void* handle;
+  return &handle;
+}
+void __hipUnregisterFatBinary(void**) {}
+void __hipRegisterFunction(void**, const void* fn, char*, const char* name, unsigned, void*, void*, void*, void*, int*) {
+  g_names.emplace_back(fn, name);
+}
+hipError_t __hipPushCallConfiguration(dim3 grid, dim3 block, size_t, hipStream_t) {
+  g_grid = grid;
+  g_block = block;
+  return hipSuccess;
+}
+hipError_t __hipPopCallConfiguration(dim3* grid, dim3* block, size_t* shared, hipStream_t* stream) {
+  *grid = g_grid;
+  *block = g_block;
+  *shared = 0;
+  *stream = nullptr;
+  return hipSuccess;
+}
+hipError_t hipLaunchKernel(const void* fn, dim3 grid, dim3 block, void** args, size_t, hipStream_t) {
+  Launch l;
+  for (auto& n : g_names)
+    if (n.first == fn) l.kernel = n.second;
+  l.grid = grid;
+  l.block = block;
+  memset(&l.args, 0, sizeof l.args);
+  if (l.kernel.find("step") == std::string::npos) l.args = *(const LinattnArgs*)args[0];
+  g_launches.push_back(l);
+  return hipSuccess;
+}
+hipError_t hipGetLastError(void) { return hipSuccess; }
+const char* hipGetErrorString(hipError_t) { return ""; }
+}
+
+static int failures = 0;
+#define EXPECT(cond, ...)                                                     \
+  do {                                                                        \
+    if (!(cond)) { printf("line %d: %s: ", __LINE__, #cond); printf(__VA_ARGS__); printf("\n"); ++failures; } \
+  } while (0)
+
+static char g_memory[64 * 256];                        // places that no call follows
+template <typename T>
+static T* at(int i) { return (T*)((((uintptr_t)g_memory + 255) / 256 + i) * 256); }
+
+static linattn_config config(int B, int T, int heads, int kv, int Dk, int Dv, int dtype, const int* offsets) {
+  linattn_config c;
+  memset(&c, 0, sizeof c);
+  c.B = B;
+  c.T = T;
+  c.heads = heads;
+  c.kv_heads = kv;
+  c.Dk = Dk;
+  c.Dv = Dv;
+  c.dtype = dtype;
+  c.scale = 1.0f;
+  c.offsets = offsets;
+  return c;
+}
+
+// One call with the workspace that it asks for (or none).
+static int call(const linattn_config& c, bool backward, float* state_in, float* state_out, bool workspace = true) {
+  int64_t bytes = 0;
+  g_launches.clear();
+  const int rc = linattn_workspace_bytes(&c, backward, &bytes);
+  if (rc != MADE_OK) return rc;
+  void* ws = workspace && bytes ? at<void>(0) : nullptr;
+  if (!backward)
+    return linattn_forward(&c, at<void>(1), at<void>(2), at<void>(3), at<float>(4), state_in, at<void>(5), state_out, ws, ws ? bytes : 0, nullptr);
+  return linattn_backward(&c, at<void>(1), at<void>(2), at<void>(3), at<float>(4), state_in, at<void>(5), at<float>(6), at<void>(7), at<void>(8),
+                          at<void>(9), state_out, ws, ws ? bytes : 0, nullptr);
+}
+
+// Where several workgroups read a sequence's state, none of them replaces it.
+static void states_in_place() {
+  int shared = 0;
+  for (int dtype : {(int)MADE_F32, (int)MADE_BF16})
+    for (bool packed : {false, true})
+      for (int group : {1, 2, 3, 8})
+        for (int kv : {1, 2, 8})
+          for (int d : {16, 64, 128})
+            for (bool workspace : {false, true}) {
+              const std::vector<int> lengths = packed ? std::vector<int>{1, 0, 64, 700, 30, 1300, 5} : std::vector<int>{900, 900};
+              std::vector<int> offsets = {0};
+              for (int n : lengths) offsets.push_back(offsets.back() + n);
+              const int B = (int)lengths.size(), T = packed ? offsets.back() : 900;
+              const linattn_config c = config(B, T, group * kv, kv, d, d, dtype, packed ? offsets.data() : nullptr);
+              float* state = at<float>(10);
+              EXPECT(call(c, false, state, state, workspace) == MADE_OK, "%s", g_error);
+              const LinattnArgs& a = g_launches.back().args;
+              if (a.q_split > 1) ++shared;
+              for (int b = 0; b < B; ++b) {
+                LinattnPlace w;
+                memset(&w, 0, sizeof w);
+                w.s.count = std::max(1, (lengths[b] + a.seg_rows - 1) / a.seg_rows);
+                w.state_at = (long long)b * kv * d * d;
+                EXPECT(a.q_split == 1 || la_state_in(a, a.role[0], w) != a.role[0].end + w.state_at,
+                       "dtype %d, packed %d, %d heads on %d states of %d, sequence of %d steps", dtype, packed, group * kv, kv, d, lengths[b]);
+              }
+            }
+  EXPECT(shared > 20, "%d calls shared a state's heads", shared);
+}
+
+int main() {
+  states_in_place();
+  printf("%d failures\n", failures);
+  return failures != 0;
+}

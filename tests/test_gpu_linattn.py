@@ -261,6 +261,20 @@ def test_state_in_place(dtype, T, B_):
     assert torch.equal(o, ref[0]) and torch.equal(state, ref[1])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,kv,D", [(8, 1, 128), (6, 2, 64)])
+def test_packed_states_in_place(dtype, heads, kv, D):
+    """sequences of one segment and of several, where workgroups share a state's query heads: as with a state for the result"""
+    c = Case(dtype, [1, 0, 64, 700, 30, 1300, 5], heads, kv, D, D, packed=True, spare=2)
+    assert B.linattn_workspace_bytes(c.B, c.T, heads, kv, D, D, DT[dtype], packed=True) > 0
+    ref = c.forward()
+    c.compare("forward", ref)
+    for _ in range(3):
+        state = c.t["s"].clone()
+        o, _ = c.forward(state_in=state, state_out=state)
+        assert torch.equal(o, ref[0]) and torch.equal(state, ref[1])
+
+
 def test_equal_calls_give_equal_bits():
     c = Case("bf16", [900] * 2, 8, 2, 128, 128)
     a, b = c.backward(), c.backward()
