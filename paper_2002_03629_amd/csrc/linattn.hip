@@ -15,6 +15,7 @@ namespace {
 constexpr int UNITS = 256;      // compute units of the device
 constexpr int MAX_T = 1 << 30;                    // positions and the ends of segments behind them stay below 2^31
 constexpr long long MAX_THREADS = 0xffffffffLL;   // of a launch
+constexpr int MAX_GRID = 65535;                   // workgroups along a launch's second and third axis
 
 int block_rows(const linattn_config& c) { return c.dtype == MADE_BF16 ? LA_BF16_ROWS : LA_F32_ROWS; }
 
@@ -48,6 +49,12 @@ struct Split {
 
 int tiles(int d) { return d <= 32 ? 1 : d <= 64 ? 2 : 4; }
 
+// Whether a walk's workgroups have fewer than 2^32 threads together.
+bool walk_fits(const linattn_config& c, long long slots, int q_split, int roles) {
+  const long long units = slots * c.kv_heads * q_split + 7;
+  return units * roles <= MAX_THREADS / ((c.dtype == MADE_BF16 ? 128 : 64) * tiles(std::max(c.Dk, c.Dv)));
+}
+
 // One workgroup for each head of a sequence, unless those fill less than the device: then the sequences are cut into
 // segments, whose sums and entering states take a second pass over keys and values and two more launches.  The number of
 // blocks to a segment is the one with the least time by what was measured (us, widths of 128, bf16 / fp32): a block of the
@@ -71,6 +78,7 @@ Split choose(const linattn_config& c, bool backward) {
     if (L == last) continue;
     last = L;
     const bool cut = L < blocks;
+    if (cut && c.kv_heads > MAX_GRID) continue;              // (of the join)
     const double slots = !cut ? c.B : c.offsets ? (double)(blocks / L + c.B) : (double)((blocks + L - 1) / L) * c.B;
     const double states = slots * heads * c.Dk * c.Dv * 4.0 * (backward ? 2 : 1);
     const double extra = !cut ? 0.0 : turns(slots * heads * (backward ? 2 : 1)) * (sums * (double)L + 2.0) + states * 3.0 / 5e6 + 8.0;
@@ -78,7 +86,7 @@ Split choose(const linattn_config& c, bool backward) {
       if (group % q != 0) continue;
       const double walk = size * (4.4 + 3.2 * (group / q - 1));
       const double cost = turns(slots * heads * q * (backward ? 3 : 1)) * (walk * (double)L + 4.0) + extra;
-      if (cost < least && slots < 1e9) {
+      if (cost < least && slots < 1e9 && walk_fits(c, (long long)slots, q, backward ? 3 : 1)) {
         least = cost;
         best.rows = cut ? (int)(L * C) : whole_rows;
         best.slots = (int)slots;
@@ -131,8 +139,12 @@ void launch_walk(int dtype, const LinattnArgs& a, bool out, hipStream_t s) {
   else vec ? launch_walk<false, true>(dtype, n, a, s) : launch_walk<false, false>(dtype, n, a, s);
 }
 
-void launch_join(const LinattnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(linattn_join_kernel, dim3((a.role[0].dk * a.role[0].dv + 255) / 256, a.kv_heads, a.B * a.roles), dim3(256), 0, s, a);
+// As many launches as the sequences of all roles need (one up to 65535 of them, unless there are very many heads).
+void launch_join(LinattnArgs& a, hipStream_t s) {
+  const int x = (a.role[0].dk * a.role[0].dv + 255) / 256;
+  const long long all = (long long)a.B * a.roles, most = std::min<long long>(MAX_GRID, MAX_THREADS / (256LL * x * a.kv_heads));
+  for (a.join0 = 0; a.join0 < all; a.join0 += most)
+    hipLaunchKernelGGL(linattn_join_kernel, dim3(x, a.kv_heads, (unsigned)std::min(most, all - a.join0)), dim3(256), 0, s, a);
 }
 
 LinattnArgs common(const linattn_config& c, const float* log_decay, const Split& s) {
@@ -163,10 +175,7 @@ int take_workspace(const char* who, const linattn_config& c, void* workspace, in
 }
 
 int check_grid(const char* who, const linattn_config& c, const Split& s, int roles) {
-  const int n = tiles(std::max(c.Dk, c.Dv));
-  const long long units = (long long)s.slots * c.kv_heads * s.q_split + 7;
-  if (units * roles > MAX_THREADS / ((c.dtype == MADE_BF16 ? 128 : 64) * n) || (s.on && ((long long)c.B * roles > 65535 || c.kv_heads > 65535)))
-    return fail(MADE_ERR_ARG, "%s: B=%d, heads=%d are more than one launch takes", who, c.B, c.kv_heads);
+  if (!walk_fits(c, s.slots, s.q_split, roles)) return fail(MADE_ERR_ARG, "%s: B=%d, heads=%d are more than one launch takes", who, c.B, c.kv_heads);
   return MADE_OK;
 }
 

@@ -68,6 +68,7 @@ struct LinattnArgs {
   int q_split;          // workgroups that share the query heads of a state (each walks the state; roles with gq > 1)
   int seg_rows;         // rows of a segment (a multiple of the block)
   int slots;            // segments in all (packed: an upper bound)
+  long long join0;      // the join: (role, sequence) pairs of the launches before
 };
 
 // lambda^n, g2 = log2 lambda (the hardware's exponential is within 1 ulp; below 2^-126 it is zero)
@@ -905,11 +906,12 @@ __global__ __launch_bounds__(64 * N, 2) void linattn_walk_f32_kernel(LinattnArgs
 }
 
 // The states that enter the segments, from what each segment adds: start[0] = the sequence's first state,
-// start[m + 1] = lambda^rows start[m] + sum[m], in place (of one segment: its copy, see la_copied).  One thread an element, grid (elements, kv heads, sequences x roles).
+// start[m + 1] = lambda^rows start[m] + sum[m], in place (of one segment: its copy, see la_copied).  One thread an element, grid (elements, kv heads, roles x sequences).
 // Bound by memory: 32 heads' 16 segments of 128 x 128 (2 x 33.5 MB) 15 us, 24 packed sequences' 128 segments of 8 heads 31 us.
 __global__ __launch_bounds__(256) void linattn_join_kernel(LinattnArgs a) {
-  const int b = blockIdx.z % a.B, head = blockIdx.y;
-  const LinattnRole& R = a.role[blockIdx.z / a.B];
+  const long long at = a.join0 + blockIdx.z;
+  const int b = (int)(at % a.B), head = blockIdx.y;
+  const LinattnRole& R = a.role[at / a.B];
   const int n = R.dk * R.dv, i = blockIdx.x * 256 + threadIdx.x;
   int len;
   const int slot = la_first_slot(a, b, len), count = min(la_count(a, len), a.slots - slot);

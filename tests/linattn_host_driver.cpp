@@ -129,8 +129,43 @@ static void states_in_place() {
   EXPECT(shared > 20, "%d calls shared a state's heads", shared);
 }
 
+// Calls of many sequences, with the workspace that they ask for, are taken, and their launches are launches: within the limits of
+// a grid, together over every state.  The states that the header promises: 8 million of width 128, 2.7 million for gradients.
+static void many_sequences() {
+  for (int backward : {0, 1})
+    for (bool packed : {true, false})
+      for (int dtype : {(int)MADE_F32, (int)MADE_BF16})
+        for (int kv : {1, 32, 70000})
+          for (int d : {16, 128})
+            for (int B : {1, 300, 21845, 21846, 32767, 32768, 65535, 65536, 70000, 250000, 2700000, 8000000})
+              for (int T : {0, 3, 200, 100000, 1 << 30}) {
+                const long long states = (long long)B * kv;
+                if (states > (backward ? 2700000 : 8000000) || (kv == 70000 && d == 128)) continue;
+                static const int offsets[1] = {0};                  // (no call looks at it)
+                const linattn_config c = config(B, T, kv, kv, d, d, dtype, packed ? offsets : nullptr);
+                const int rc = call(c, backward, nullptr, at<float>(10));
+                EXPECT(rc == MADE_OK, "%d sequences, %d steps, %d heads of %d, packed %d, dtype %d, backward %d: %s", B, T, kv, d, packed, dtype, backward, g_error);
+                if (rc != MADE_OK) continue;
+                const LinattnArgs& walk = g_launches.back().args;
+                EXPECT(walk.roles == (backward ? 3 : 1) && (long long)walk.slots * kv * walk.q_split * walk.roles <= g_launches.back().grid.x, "%d sequences", B);
+                long long joined = 0;
+                bool join = false;
+                for (const Launch& l : g_launches) {
+                  EXPECT(l.grid.y <= 65535 && l.grid.z <= 65535 && l.grid.x > 0 && l.grid.y > 0 && l.grid.z > 0 &&
+                             (double)l.grid.x * l.grid.y * l.grid.z * l.block.x < 4294967296.0,
+                         "%s: %u x %u x %u workgroups", l.kernel.c_str(), l.grid.x, l.grid.y, l.grid.z);
+                  if (l.kernel.find("join") == std::string::npos) continue;
+                  join = true;
+                  EXPECT(l.args.join0 == joined && (int)l.grid.x * 256 >= d * d && (int)l.grid.y == kv, "%lld joined", joined);
+                  joined += l.grid.z;
+                }
+                EXPECT(joined == (join ? (long long)B * (backward ? 2 : 1) : 0) && (packed || !join || walk.seg_rows < T), "%lld joined", joined);
+              }
+}
+
 int main() {
   states_in_place();
+  many_sequences();
   printf("%d failures\n", failures);
   return failures != 0;
 }

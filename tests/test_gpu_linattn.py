@@ -408,6 +408,36 @@ def test_more_sequences_than_a_cut_call_may_have(dtype):
         last.compare(fn, [x[-5:] for x in all_])
 
 
+@pytest.mark.parametrize("dtype,B_", [("f32", 34000), ("bf16", 70000)])
+def test_more_packed_sequences_than_one_join_takes(dtype, B_):
+    """a few long sequences, which are cut, among very many of a step or none; in gradients 68000 and 140000 pairs of a state and a
+    role.  The long ones and the ends are those of a call of their own, the others those of an uncut call."""
+    lengths = [(i * 7919) % 3 % 2 for i in range(B_)]
+    long_ = {0: 400, 21846: 333, 33000: 1000, B_ - 1: 500}
+    for b, n in long_.items():
+        lengths[b] = n
+    c = Case(dtype, lengths, 2, 1, 16, 16, packed=True, spare=3)
+    only = sorted([*long_, 1, 21845, 32999, B_ - 2])
+    at = np.concatenate([[0], np.cumsum(lengths)])
+    rows = np.concatenate([np.arange(at[b], at[b + 1]) for b in only])
+    few = Case(dtype, [lengths[b] for b in only], 2, 1, 16, 16, packed=True)
+    for key in ("q", "k", "v", "do", "s", "ds"):
+        pick = only if key in ("s", "ds") else rows
+        few.t[key].copy_(c.t[key][pick])
+        few.x[key] = c.x[key][pick]
+    short = np.setdiff1d(np.arange(at[-1]), np.concatenate([np.arange(at[b], at[b + 1]) for b in long_]))
+    for fn, back in (("forward", False), ("backward", True)):
+        need = B.linattn_workspace_bytes(c.B, c.T, 2, 1, 16, 16, DT[dtype], packed=True, backward=back)
+        assert need > 0
+        cut = getattr(c, fn)(torch.empty(need, dtype=torch.uint8, device="cuda"))
+        whole = getattr(c, fn)(torch.empty(256, dtype=torch.uint8, device="cuda"))
+        few.compare(fn, [x[rows] for x in cut[:-1]] + [cut[-1][only]])
+        for x, y in zip(cut[:-1], whole[:-1]):
+            assert torch.equal(x[short], y[short]) and (c.spare(x) == 7).all()
+        others = np.setdiff1d(np.arange(B_), list(long_))
+        assert torch.equal(cut[-1][others], whole[-1][others])
+
+
 def test_two_calls_at_once():
     """on two streams, a workspace each"""
     c = [Case("bf16", [3000], 4, 2, 64, 64, seed=i) for i in range(2)]
