@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "entry.hpp"
 #include "linattn.hpp"
@@ -179,6 +180,17 @@ int check_grid(const char* who, const linattn_config& c, const Split& s, int rol
   return MADE_OK;
 }
 
+// Arrays that a call writes are none of those that it reads, and no two of them are one (by their addresses; NULL: absent).
+int check_apart(const char* who, const char* written, std::initializer_list<const void*> out, std::initializer_list<const void*> in) {
+  for (const void* const* x = out.begin(); x != out.end(); ++x) {
+    for (const void* y : in)
+      if (*x && *x == y) return fail(MADE_ERR_ARG, "%s: %s is one of the inputs", who, written);
+    for (const void* const* y = x + 1; y != out.end(); ++y)
+      if (*x && *x == *y) return fail(MADE_ERR_ARG, "%s: two gradients, outputs or workspaces are one array", who);
+  }
+  return MADE_OK;
+}
+
 }  // namespace
 
 extern "C" int linattn_workspace_bytes(const linattn_config* cfg, int32_t backward, int64_t* bytes) {
@@ -196,7 +208,9 @@ extern "C" int linattn_forward(const linattn_config* cfg, const void* q, const v
   const linattn_config& c = *cfg;
   if (c.B == 0) return MADE_OK;
   if (!log_decay || (c.T > 0 && (!q || !k || !v || !o))) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
-  if (o && (o == q || o == k || o == v)) return fail(MADE_ERR_ARG, "%s: o is one of the inputs", who);
+  const void* ws = workspace_bytes > 0 ? workspace : nullptr;
+  TRY(check_apart(who, "an output", {o, ws}, {q, k, v, log_decay, state_in, c.offsets}));
+  TRY(check_apart(who, "state_out", {state_out, o, ws}, {q, k, v, log_decay, c.offsets}));      // (it may be state_in)
   Split split = choose(c, false);
   TRY(take_workspace(who, c, workspace, workspace_bytes, 1, split));
   TRY(check_grid(who, c, split, 1));
@@ -238,12 +252,8 @@ extern "C" int linattn_backward(const linattn_config* cfg, const void* q, const 
   if (c.B == 0) return MADE_OK;
   if (!log_decay || (c.T > 0 && (!q || !k || !v || !d_o || !dq || !dk || !dv))) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
   if (d_state_in && d_state_in == d_state_out) return fail(MADE_ERR_ARG, "%s: d_state_in is d_state_out", who);
-  const void *in[4] = {q, k, v, d_o}, *out[3] = {dq, dk, dv};
-  for (int i = 0; i < 3; ++i) {
-    for (int j = 0; j < 4; ++j)
-      if (out[i] && out[i] == in[j]) return fail(MADE_ERR_ARG, "%s: a gradient is one of the inputs", who);
-    if (out[i] && out[i] == out[(i + 1) % 3]) return fail(MADE_ERR_ARG, "%s: two gradients are one array", who);
-  }
+  TRY(check_apart(who, "a gradient or the workspace", {dq, dk, dv, d_state_in, workspace_bytes > 0 ? workspace : nullptr},
+                  {q, k, v, d_o, log_decay, state_in, d_state_out, c.offsets}));
   Split split = choose(c, true);
   TRY(take_workspace(who, c, workspace, workspace_bytes, 2, split));
   TRY(check_grid(who, c, split, 3));
@@ -321,7 +331,7 @@ extern "C" int linattn_step(const linattn_config* cfg, const void* q, const void
   if (n_slots < 0 || (!slots && n_slots < c.B)) return fail(MADE_ERR_ARG, "%s: n_slots=%d, B=%d", who, n_slots, c.B);
   if (c.B == 0) return MADE_OK;
   if (!q || !k || !v || !log_decay || !state || !o) return fail(MADE_ERR_ARG, "%s: NULL argument", who);
-  if (o == q || o == k || o == v) return fail(MADE_ERR_ARG, "%s: o is one of the inputs", who);
+  TRY(check_apart(who, "o or the state", {o, state}, {q, k, v, log_decay, slots}));
   LinattnStepArgs a;
   a.q = view(q, c.ld_q, c.heads, c.Dk);
   a.k = view(k, c.ld_k, c.kv_heads, c.Dk);

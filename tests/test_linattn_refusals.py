@@ -86,6 +86,38 @@ def test_an_output_that_is_an_input():
         assert refused(L.linattn_backward(C.byref(config()), *q[:4], None, q[4], None, *grads, None, None, 0, None), "two gradients")
 
 
+def test_states_workspaces_and_small_arrays_that_are_another_array():
+    """every array a call writes against every other one, at its own address; a state alone may be replaced in place"""
+    L, off = B.lib(), 4096 * 40
+    cfg = config(T=5000, offsets=off)                                    # (long enough to be cut: the workspace is used)
+    names = ["q", "k", "v", "log_decay", "state_in", "o", "state_out", "workspace"]
+    back = ["q", "k", "v", "log_decay", "state_in", "d_o", "d_state_out", "dq", "dk", "dv", "d_state_in", "workspace"]
+    step = ["q", "k", "v", "log_decay", "state", "slots", "o"]
+    fresh = lambda ns: {n: 4096 * (i + 1) for i, n in enumerate(ns)}
+
+    def forward(p):
+        return L.linattn_forward(C.byref(cfg), *(p[n] for n in names), 1 << 30, None)
+
+    def backward(p):
+        return L.linattn_backward(C.byref(cfg), *(p[n] for n in back), 1 << 30, None)
+
+    def one_step(p):
+        return L.linattn_step(C.byref(cfg), *(p[n] for n in step[:5]), 2, p["slots"], p["o"], None)
+
+    for call, ns, written in ((forward, names, ("o", "state_out", "workspace")), (one_step, step, ("state", "o")),
+                              (backward, back, ("dq", "dk", "dv", "d_state_in", "workspace"))):
+        for w in written:
+            for other in ns:
+                if other == w or (call is forward and {w, other} == {"state_in", "state_out"}):
+                    continue
+                p = fresh(ns)
+                p[w] = p[other]
+                assert call(p) == B.MADE_ERR_ARG, (w, other)
+                assert any(x in B.made_last_error() for x in ("inputs", "one array", "d_state_out")), (w, other, B.made_last_error())
+            if call is not one_step:
+                assert call({**fresh(ns), w: off}) == B.MADE_ERR_ARG, w
+
+
 def test_the_binding_refuses_other_types():
     with pytest.raises(ValueError, match="float16"):
         B.linattn_workspace_bytes(1, 64, 4, 2, 16, 16, torch.float16)
