@@ -618,10 +618,8 @@ class PreparedAdamW:
         spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in written)
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("two of the tensors that are written overlap (is one listed twice?)")
-        self._cfg = adamw_config()
-        self._cfg.param_dtype = MADE_BF16 if params[0].dtype == torch.bfloat16 else MADE_F32
-        self._cfg.grad_dtype = MADE_BF16 if grads[0].dtype == torch.bfloat16 else MADE_F32
-        self._cfg.moment_bits = 8 if eight else 32
+        self._types = (MADE_BF16 if params[0].dtype == torch.bfloat16 else MADE_F32,
+                       MADE_BF16 if grads[0].dtype == torch.bfloat16 else MADE_F32, 8 if eight else 32)
         self._keep = (params, grads, m, v, m_scale, v_scale, copies)
         self._fn = lib().adamw_step
 
@@ -630,8 +628,7 @@ class PreparedAdamW:
         """scalars: float64 [4] on the device, {lr, 1 / (1 - beta1^step), 1 / (1 - beta2^step), grad_scale}, read when the step
         runs in place of lr, step and grad_scale (a recorded step then follows them), or None."""
         import torch
-        c = self._cfg
-        c.lr, c.beta1, c.beta2, c.eps, c.weight_decay, c.grad_scale, c.step = lr, beta1, beta2, eps, weight_decay, grad_scale, step
+        c = adamw_config(lr, beta1, beta2, eps, weight_decay, grad_scale, step, *self._types)     # (the call's own: threads may share the object)
         if any(self._device.index != d for d in (torch.cuda.current_device(), *([] if stream is None else [stream.device.index]))):
             raise ValueError(f"the tensors are on {self._device}, the call is for another device")
         _check(self._fn(C.byref(c), self._n, self._sizes, *self._arrays, _dense(scalars, "scalars", (4,), torch.float64, stream),

@@ -82,3 +82,24 @@ def test_zeroed_moments():
     m, v, ms, vs = B.adamw_moments([torch.zeros(3, 100), torch.zeros(1)], 8)
     assert [x.dtype for x in (m[0], v[0], ms[0], vs[0])] == [torch.int8, torch.uint8, torch.float32, torch.float32]
     assert [x.shape for x in m] == [(3, 100), (1,)] and [x.numel() for x in ms] == [2, 1]
+
+
+def test_calls_of_one_prepared_step_have_their_own_numbers(monkeypatch):
+    """a call made while another of the same object is under way (two threads) does not change the other's numbers"""
+    seen = []
+
+    class Library:
+        @staticmethod
+        def adamw_step(cfg, *args):
+            if cfg._obj.step == 1:
+                plan(2.0, 0.8, 0.8, 1.0, 0.0, 2, 0.5)
+            seen.append((cfg._obj.lr, cfg._obj.beta1, cfg._obj.step, cfg._obj.grad_scale, cfg._obj.moment_bits))
+            return B.MADE_OK
+
+    monkeypatch.setattr(B, "_on_device", lambda t, *a: t)              # (tensors of the host, a library that computes nothing)
+    monkeypatch.setattr(B, "_stream", lambda s: None)
+    monkeypatch.setattr(B, "lib", Library)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: None)
+    plan = B.PreparedAdamW(*[[torch.zeros(4)] for _ in range(4)])
+    plan(1.0, 0.9, 0.9, 1.0, 0.0, 1)
+    assert seen == [(2.0, 0.8, 2, 0.5, 32), (1.0, 0.9, 1, 1.0, 32)]
