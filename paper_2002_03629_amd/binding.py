@@ -539,6 +539,7 @@ class PreparedLinattnStep:
         pv, lv = _rows(v, "v", (B,), kv_heads, Dv, q.dtype, stream)
         po, lo = _rows(o, "o", (B,), heads, Dv, q.dtype, stream)
         n_slots = state.shape[0]
+        self._device, self._current = q.device.index, torch.cuda.current_device
         self._keep = (q, k, v, log_decay, state, slots, o, stream)
         self._cfg = linattn_config(int(B), 1, int(heads), int(kv_heads), int(Dk), int(Dv), code, float(scale), lq, lk, lv, lo, None)
         self._fn = lib().linattn_step
@@ -548,6 +549,8 @@ class PreparedLinattnStep:
                       vp(_dense(slots, "slots", (B,), torch.int32, stream)), vp(po), vp(_stream(stream)))
 
     def __call__(self) -> None:
+        if self._current() != self._device:      # (a launch goes to the current device whatever its tensors)
+            raise ValueError(f"the tensors are on cuda:{self._device}, the current device is cuda:{self._current()}")
         code = self._fn(*self._args)
         if code != MADE_OK:
             raise MadeError(code, made_last_error())

@@ -137,6 +137,31 @@ def test_the_binding_refuses_a_stream_of_another_device(monkeypatch):
             B._on_device(Of(t), "x", None if s is None else Of(s))
 
 
+def test_a_prepared_step_refuses_another_current_device(monkeypatch):
+    calls = []
+
+    class Library:
+        @staticmethod
+        def linattn_step(*args):
+            calls.append(args)
+            return B.MADE_OK
+
+    device = [None]                                                    # (tensors of the host, a library that computes nothing)
+    monkeypatch.setattr(B, "_on_device", lambda t, *a: t)
+    monkeypatch.setattr(B, "_stream", lambda s: None)
+    monkeypatch.setattr(B, "lib", Library)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: device[0])
+    x, state = torch.zeros(1, 2, 4), torch.zeros(1, 2, 4, 4)
+    step = B.PreparedLinattnStep(x, x, x, torch.zeros(2), state, None, 1, 2, 2, 4, 4, 1.0, torch.zeros(1, 2, 4))
+    step()
+    device[0] = 1
+    with pytest.raises(ValueError, match="cuda:1"):
+        step()
+    device[0] = None
+    step()
+    assert len(calls) == 2
+
+
 def test_an_empty_batch_needs_no_pointers():
     L = B.lib()
     c = C.byref(config(B=0))
