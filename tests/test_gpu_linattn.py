@@ -208,6 +208,27 @@ def test_bf16_outputs_are_off_by_little_more_than_their_own_rounding(dtype):
         assert (err <= tol).all()
 
 
+@pytest.mark.parametrize("decay", ["mixed", "none"])
+@pytest.mark.parametrize("lengths,heads,kv,Dk,Dv,packed", [([300], 2, 2, 128, 128, False), ([1100], 4, 1, 128, 64, False), ([90, 90], 6, 2, 40, 72, False),
+                                                           ([700, 3, 0, 450, 64], 4, 2, 64, 96, True)])
+def test_bf16_outputs_and_gradients_with_states(lengths, heads, kv, Dk, Dv, packed, decay):
+    """As above, for gradients too, with states that enter and their gradients, cut and whole.  A term that reaches an output through a
+    block's scores is rounded to two bf16 parts once; one that reaches it through the state twice: as a decayed value and where the
+    state is read (whose value a segment's sum and the state that enters have their share in).  Each is off by 2^-17 of the
+    term at most: a part's rounding is half a step of 2^-7, the first one's rest is below 2^-8 of the value, a half step of it
+    2^-8 of that, and of the rest's own binade half again."""
+    c = Case("bf16", lengths, heads, kv, Dk, Dv, decay=decay, packed=packed, spare=2 if packed else 0, seed=heads)
+    for fn in ("forward", "backward"):
+        for n in (1 << 24, 256):
+            got = getattr(c, fn)(workspace=torch.empty(n, dtype=torch.uint8, device="cuda"))
+            for b in range(c.B):
+                ref, mag = c.oracle(fn, b), c.oracle(fn, b, True)
+                for i in range(len(ref) - 1):
+                    err = np.abs(got[i][c.rows(b)].double().cpu().numpy() - ref[i])
+                    tol = (c.roundings(lengths[b]) * 2.0 ** -24 + 3 * 2.0 ** -17) * mag[i] + 2.0 ** -8 * np.abs(ref[i])
+                    assert (err <= tol).all(), (fn, n, b, i, (err / tol).max())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_no_carried_state(dtype):
     c = Case(dtype, [140] * 2, 2, 2, 64, 64, carry=False)
