@@ -96,10 +96,18 @@ __device__ __forceinline__ void la_rows(const LinattnArgs& a, int b, int& row0, 
   len = min(max(a.offsets[b + 1], lo), a.T) - lo;
 }
 
-__device__ __forceinline__ int la_count(const LinattnArgs& a, int len) { return max(1, (len + a.seg_rows - 1) / a.seg_rows); }
+__host__ __device__ __forceinline__ int la_count(const LinattnArgs& a, int len) { return len <= a.seg_rows ? 1 : (len + a.seg_rows - 1) / a.seg_rows; }
 
-// The segment with number `slot` (false: there are fewer).  Packed sequences: every wave adds up the counts of 64
-// sequences at a time.
+// Number of the first segment of sequence b, whose rows begin at row0.  Cut packed sequences (R rows to a segment): none has
+// more segments than floor(row0 / R) + b grows by to the next one (ceil(n / R) <= floor((row0 + n) / R) - floor(row0 / R) + 1),
+// so that no sum over those before is needed; numbers between are no segment's.
+__host__ __device__ __forceinline__ int la_first_slot(const LinattnArgs& a, int b, int row0) {
+  return !a.offsets ? b * la_count(a, a.T) : a.seg_rows < a.T ? row0 / a.seg_rows + b : b;
+}
+
+// The segment with number `slot` (false: there is none).  Cut packed sequences: the last one whose first segment is not behind
+// `slot`, searched by every wave, 64 candidates at a time, then 64 among those up to the next (a sum of the counts before
+// took 260 ms in all for 65536 sequences of 8 rows).
 __device__ __forceinline__ bool la_find(const LinattnArgs& a, int slot, LinattnSegment& s) {
   if (!a.offsets) {
     s.count = la_count(a, a.T);
@@ -110,50 +118,29 @@ __device__ __forceinline__ bool la_find(const LinattnArgs& a, int slot, LinattnS
     return s.b < a.B;
   }
   const int lane = threadIdx.x & 63;
-  int base = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    int row0 = 0, len = 0, n = 0;
-    if (b0 + lane < a.B) {
-      la_rows(a, b0 + lane, row0, len);
-      n = la_count(a, len);
+  const bool cut = a.seg_rows < a.T;
+  int lo = cut ? 0 : slot, n = cut ? a.B : 1;
+  while (true) {
+    const int step = (n + 63) / 64;
+    int row0 = 0, len = 0;
+    bool here = false;
+    if (lane * step < n) {
+      la_rows(a, lo + lane * step, row0, len);
+      here = la_first_slot(a, lo + lane * step, row0) <= slot;
     }
-    int incl = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int up = __shfl_up(incl, d);
-      if (lane >= d) incl += up;
-    }
-    const unsigned long long hit = __ballot(slot < base + incl);
-    if (hit) {
-      const int f = __ffsll((long long)hit) - 1;
-      s.b = b0 + f;
-      s.count = __builtin_amdgcn_readfirstlane(__shfl(n, f));
-      s.index = slot - base - (__builtin_amdgcn_readfirstlane(__shfl(incl, f)) - s.count);
-      s.row0 = __builtin_amdgcn_readfirstlane(__shfl(row0, f));
-      s.len = __builtin_amdgcn_readfirstlane(__shfl(len, f));
-      return true;
-    }
-    base += __builtin_amdgcn_readfirstlane(__shfl(incl, 63));
+    const unsigned long long hit = __ballot(here);
+    if (!hit) return false;
+    const int f = 63 - __clzll((long long)hit);
+    lo += f * step;
+    n = min(step, n - f * step);
+    if (step > 1) continue;
+    s.b = lo;
+    s.row0 = __builtin_amdgcn_readfirstlane(__shfl(row0, f));
+    s.len = __builtin_amdgcn_readfirstlane(__shfl(len, f));
+    s.count = la_count(a, s.len);
+    s.index = slot - la_first_slot(a, lo, s.row0);
+    return s.index < s.count;
   }
-  return false;
-}
-
-// Number of the first segment of sequence b, and its rows.
-__device__ __forceinline__ int la_first_slot(const LinattnArgs& a, int b, int& len) {
-  if (!a.offsets) {
-    len = a.T;
-    return b * la_count(a, a.T);
-  }
-  const int lane = threadIdx.x & 63;
-  int n = 0, row0 = 0;
-  for (int i = lane; i < b; i += 64) {
-    la_rows(a, i, row0, len);
-    n += la_count(a, len);
-  }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
-  la_rows(a, b, row0, len);
-  return n;
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -913,8 +900,9 @@ __global__ __launch_bounds__(256) void linattn_join_kernel(LinattnArgs a) {
   const int b = (int)(at % a.B), head = blockIdx.y;
   const LinattnRole& R = a.role[at / a.B];
   const int n = R.dk * R.dv, i = blockIdx.x * 256 + threadIdx.x;
-  int len;
-  const int slot = la_first_slot(a, b, len), count = min(la_count(a, len), a.slots - slot);
+  int row0 = 0, len = a.T;
+  if (a.offsets) la_rows(a, b, row0, len);
+  const int slot = la_first_slot(a, b, row0), count = min(la_count(a, len), a.slots - slot);
   if (i >= n || count < (la_copied(a, R) ? 1 : 2)) return;
   const float f = la_pow(a.log_decay[head] * 1.44269504088896340736f, a.seg_rows);
   float* p = R.seg + ((long long)slot * a.kv_heads + head) * n + i;

@@ -163,8 +163,33 @@ static void many_sequences() {
               }
 }
 
+// Every segment of a packed call has a number of its own, below the number of those that the call has room for.
+static void segment_numbers() {
+  unsigned seed = 1;
+  auto draw = [&](int n) { return (int)((seed = seed * 1664525u + 1013904223u) >> 8) % n; };
+  int cut = 0;
+  for (int rep = 0; rep < 400; ++rep) {
+    const int B = 1 + draw(rep % 4 ? 40 : 900), most = 1 << draw(12);
+    std::vector<int> offsets = {draw(3)};
+    for (int b = 0; b < B; ++b) offsets.push_back(offsets.back() + (draw(3) ? draw(most) : draw(2) * 64));
+    const linattn_config c = config(B, offsets.back() + draw(2) * draw(200), 2, 2, 32, 32, rep % 2 ? MADE_BF16 : MADE_F32, offsets.data());
+    EXPECT(call(c, rep / 2 % 2, nullptr, at<float>(10)) == MADE_OK, "%s", g_error);
+    const LinattnArgs& a = g_launches.back().args;
+    cut += a.role[0].seg != nullptr;
+    int next = 0;
+    for (int b = 0; b < B; ++b) {
+      const int first = la_first_slot(a, b, offsets[b]);
+      EXPECT(first >= next && (a.role[0].seg || first == b), "sequence %d of %d", b, B);
+      next = first + la_count(a, offsets[b + 1] - offsets[b]);
+    }
+    EXPECT(next <= a.slots, "%d of %d", next, a.slots);
+  }
+  EXPECT(cut > 100, "%d calls were cut", cut);
+}
+
 int main() {
   states_in_place();
+  segment_numbers();
   many_sequences();
   printf("%d failures\n", failures);
   return failures != 0;

@@ -459,6 +459,33 @@ def test_more_packed_sequences_than_one_join_takes(dtype, B_):
         assert torch.equal(cut[-1][others], whole[-1][others])
 
 
+@pytest.mark.parametrize("cut", [False, True])
+def test_a_million_packed_sequences(cut):
+    """of a step or none, one long sequence among them: in a time that does not grow with the square of their number"""
+    n, D, g = 1 << 20, 8, np.random.default_rng(2)
+    lengths = g.integers(0, 2, n)
+    lengths[n // 2] = 300
+    at = np.concatenate([[0], np.cumsum(lengths)])
+    T, i = int(at[-1]), int(at[n // 2])
+    q, k, v = (torch.from_numpy(g.normal(size=(T, 1, D)).astype(np.float32)).cuda() for _ in range(3))
+    ld, offsets = torch.full((1,), -0.1, device="cuda"), torch.from_numpy(at.astype(np.int32)).cuda()
+    need = B.linattn_workspace_bytes(n, T, 1, 1, D, D, torch.float32, packed=True) if cut else 256
+    ws, o, end = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty_like(v), torch.empty(n, 1, D, D, device="cuda")
+    B.linattn_forward(q, k, v, ld, None, offsets, n, T, 1, 1, D, D, 0.5, o, end, workspace=ws)
+    q, k, v, o, end = (x.double().cpu().numpy()[:, 0] for x in (q, k, v, o, end))
+    # a step alone: 8 products and sums, a factor; the state after it is the product
+    one = np.setdiff1d(np.arange(T), np.arange(i, i + 300))
+    ref, mag = 0.5 * (q * k).sum(1, keepdims=True) * v, 0.5 * np.abs(q * k).sum(1, keepdims=True) * np.abs(v)
+    assert (np.abs(o - ref) <= 24 * 2.0 ** -24 * mag)[one].all()
+    whose = np.repeat(np.arange(n), lengths)[one]
+    assert (np.abs(end[whose] - k[one][:, :, None] * v[one][:, None, :]) <= 2 * 2.0 ** -24 * np.abs(end[whose])).all()
+    assert not end[lengths == 0].any()
+    ref, last, _ = L.forward(*(x[i:i + 300, None] for x in (q, k, v)), np.array([np.float32(-0.1)]), 0.5)
+    mag, m_last, _ = L.forward(*(np.abs(x[i:i + 300, None]) for x in (q, k, v)), np.array([np.float32(-0.1)]), 0.5)
+    tol = (2 * D + 64 + 4 * 10 + 2 * 45 + 16) * 2.0 ** -24
+    assert (np.abs(o[i:i + 300] - ref[:, 0]) <= tol * mag[:, 0]).all() and (np.abs(end[n // 2] - last[0]) <= tol * m_last[0]).all()
+
+
 def test_two_calls_at_once():
     """on two streams, a workspace each"""
     c = [Case("bf16", [3000], 4, 2, 64, 64, seed=i) for i in range(2)]
