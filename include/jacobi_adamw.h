@@ -12,6 +12,7 @@
  * the nearest root (halves up), a second moment that is not zero never code 0, so that a step is not divided by eps alone.  All
  * zero bytes and scales are moments of zero.  m and v are computed in 64 bits from their codes and rounded once, to codes;
  * the step takes them as fp32 before that.  A block with a moment that is not finite has the scale NaN, and reads as NaN.
+ * Moments in 32 bits are formed in fp32: the square of a g beyond 2^64 is infinite there, and its weight then only decays.
  *
  * Conventions (as in jacobi_rnn.h): the arrays of pointers and sizes are HOST memory, read during the call; what they
  * point to is DEVICE memory, contiguous, owned by the caller, and no two of the buffers written may overlap.  Calls are

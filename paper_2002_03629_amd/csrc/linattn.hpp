@@ -9,12 +9,11 @@
 // blocks of C steps: the state stays in accumulator registers, divided among the waves by value columns, the block's q, k, v
 // pass through LDS, the next block's are requested before the products of this one.
 //
-// What it costs (one sequence of 32768 steps, 32 heads, widths of 128, bf16, 16 segments to a head: 412 us in all with calls in
-// a row, 1.07 GB of q, k, v and o take 221 at the 4.85 TB/s that a copy of 2 GiB reaches; a kernel trace shows each launch
-// somewhat longer than in a row): the walk 299 us, 4.6 us of a compute unit for a block's 64 KB (3.5 at the copy's rate); by
-// the counters the SIMDs issue vector instructions 54 % and run MFMAs 33 % of the time (issue cycles and busy cycles over
-// those of the shader engines), LDS is read or written 40 %.  Vector and matrix time added up in every variant timed, so fewer
-// instructions is what has paid.  The pass for the sums 133 us, 2.1 us a block's 32 KB (1.7), 51 % and 25 %.
+// What it costs (one sequence of 32768 steps, 32 heads, widths of 128, bf16, 16 segments to a head: 410 us in all with calls in
+// a row, 1.07 GB of q, k, v and o take 172 at the 6.26 TB/s that an elementwise product of 8 GiB reaches): the walk 287 us, 4.5 us
+// of a compute unit for a block's 64 KB (2.7 at that rate); by the counters the SIMDs issue vector instructions 55 % and run
+// MFMAs 34 % of the time (issue cycles and busy cycles over those of the shader engines), LDS is read or written 40 %.  Vector and matrix time added up in every variant timed, so fewer
+// instructions is what has paid.  The pass for the sums 140 us, 2.2 us a block's 32 KB (1.3), 52 % and 25 %.
 //
 // The gradients are the same recurrence with the arrays in other roles, so the same kernel computes them:
 //     dq: queries do, keys v, values k, forward in time, the states of the forward pass (transposed)
@@ -658,8 +657,8 @@ __global__ __launch_bounds__(128 * N, N == 4 ? 4 : 2) void linattn_walk_bf16_ker
 // over).  Wave w holds the value columns 32 w .. 32 w + 31.
 //
 // Bound by the chain of a block's products, not by memory: 3 x 1777 steps of 6 heads, widths 72 and 100, one workgroup to a
-// unit, one wave to a SIMD: the walk 37 us (MFMAs 42 %, vector issue 11 % of the time), the pass for the sums 18, the join 5;
-// the 45 MB take 9 at the copy's rate.
+// unit, one wave to a SIMD: the walk 36 us (MFMAs 42 %, vector issue 11 % of the time), the pass for the sums 18, the join 5;
+// the 45 MB take 7.2 at 6.26 TB/s.
 template <int KT, bool OUT>
 struct LaLdsF32 {
   static constexpr int PITCH = KT * 32 + 4, VPITCH = PITCH;
@@ -893,7 +892,8 @@ __global__ __launch_bounds__(64 * N, 2) void linattn_walk_f32_kernel(LinattnArgs
 }
 
 // The states that enter the segments, from what each segment adds: start[0] = the sequence's first state,
-// start[m + 1] = lambda^rows start[m] + sum[m], in place (of one segment: its copy, see la_copied).  One thread an element, grid (elements, kv heads, roles x sequences).
+// start[m + 1] = lambda^rows start[m] + sum[m], in place (of one segment: its copy, see la_copied).  One thread an element, grid
+// (elements, kv heads, roles x sequences).
 // Bound by memory: 32 heads' 16 segments of 128 x 128 (2 x 33.5 MB) 15 us, 24 packed sequences' 128 segments of 8 heads 31 us.
 __global__ __launch_bounds__(256) void linattn_join_kernel(LinattnArgs a) {
   const long long at = a.join0 + blockIdx.z;
